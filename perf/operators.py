@@ -239,10 +239,10 @@ def _norm(s):
 
 
 def _sample(s):
-    """The kept choices are a prefix of the order by (logit descending, index ascending): at most top_k of them, the
+    """The choices in the order (logit descending, index ascending).  Kept is a prefix: at most top_k of them, the
     shortest prefix that holds top_p of the top-k choices' mass, and only those with at least min_p of the largest
-    one's probability.  The choice is the first, by index, whose running sum of kept probabilities exceeds the uniform;
-    a row without any has the choice -1."""
+    one's probability.  The choice is the first in that order whose running sum of kept probabilities exceeds the
+    uniform; a row without any has the choice -1."""
     x = s["logits"].double()
     V = x.shape[1]
     greedy = ~(s["temperature"] > 0)[:, None]
@@ -264,11 +264,12 @@ def _sample(s):
         keep = keep & ((before < p * held.sum(1, keepdim=True)) | (p >= 1) | (rank == 0))
     if s["min_p"] is not None:
         keep = keep & (mass >= s["min_p"][:, None].double())
-    kept = torch.zeros_like(x).scatter_(1, index, mass * keep)
+    kept = mass * keep
     run = torch.cumsum(kept, 1)
     total = run[:, -1:]
-    token = (run <= s["uniforms"][:, None].double() * total).sum(1, keepdim=True).clamp_max(V - 1)
-    logprob = torch.where(empty, -math.inf, torch.log(torch.gather(kept, 1, token) / total))
+    at = (run <= s["uniforms"][:, None].double() * total).sum(1, keepdim=True).clamp_max(V - 1)
+    token = torch.gather(index, 1, at)
+    logprob = torch.where(empty, -math.inf, torch.log(torch.gather(kept, 1, at) / total))
     return torch.where(empty, -1, token)[:, 0].to(torch.int32), logprob[:, 0].float()
 
 
@@ -348,7 +349,7 @@ def _exact_sample(s):
             most = 1 + int(np.searchsorted(sums[:-1], top_p[r] * sums[-1], side="left"))
         if min_p is not None:
             most = max(1, min(most, int(np.count_nonzero(prob[order] >= min_p[r]))))
-        kept = np.sort(order[:most])
+        kept = order[:most]
         sums = np.cumsum(prob[kept])
         at = min(int(np.searchsorted(sums, u[r] * sums[-1], side="right")), kept.size - 1)
         tokens.append(int(kept[at]))
