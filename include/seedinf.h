@@ -165,7 +165,7 @@ seed_status_t seed_infer_step(seed_infer_t* handle, int32_t B,
                               void* hip_stream);
 
 /*
- * The step with episode boundaries and epsilon-greedy exploration.
+ * The step with episode boundaries, epsilon-greedy exploration and filtered sampling.
  *
  * Section 3 ("Detailed Learner architecture"): the inference thread receives
  * episode termination flags with the observations; Appendix A.3.1 (agent
@@ -185,16 +185,31 @@ seed_status_t seed_infer_step(seed_infer_t* handle, int32_t B,
  *                     action min(floor(u1 * num_actions), num_actions - 1)
  *                     instead.  logits_out, value_out and probs_out are
  *                     unaffected.  The two must be given together.
+ *   sample_uniforms   [B] fp32 uniforms in [0, 1): the action is drawn from
+ *                     logits_out (Q-values for a dueling head) by
+ *                     seed_op_sample instead of the arch's own selection, with
+ *   temperature, top_k, top_p, min_p   [B] each, as for seed_op_sample; they
+ *                     need sample_uniforms.  `uniforms` must then be NULL
+ *                     whatever the arch's selection, and epsilon absent.
+ *                     logits_out, value_out and probs_out are unaffected.
  *
- * Set struct_size = sizeof(seed_step_ext_t).  Everything else (arguments,
- * stream behaviour, error returns) is as for seed_infer_step.
+ * Set struct_size = sizeof(seed_step_ext_t); SEED_STEP_EXT_SIZE_EPISODE, the
+ * size up to and with explore_uniforms, is accepted too, the fields behind it
+ * being absent.  Everything else (arguments, stream behaviour, error returns)
+ * is as for seed_infer_step.
  */
 typedef struct seed_step_ext {
     uint32_t struct_size;
     const uint8_t* done;
     const float* epsilon;
     const float* explore_uniforms;
+    const float* sample_uniforms;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
 } seed_step_ext_t;
+#define SEED_STEP_EXT_SIZE_EPISODE (offsetof(seed_step_ext_t, sample_uniforms))
 
 seed_status_t seed_infer_step_ext(seed_infer_t* handle, int32_t B,
                                   const uint8_t* obs,
@@ -386,6 +401,137 @@ void* seed_batcher_stream(seed_batcher_t* b);
 const char* seed_batcher_last_error(const seed_batcher_t* b);
 /* Waits for work in flight and frees the batcher.  NULL is allowed. */
 void seed_batcher_destroy(seed_batcher_t* b);
+
+/* ------------------------------------------------------------------------
+ * Stand-alone operators: a recurrent core, a normalisation and a sampler for
+ * agents whose network a caller composes beside (or behind) a seed_infer
+ * handle.  Forward passes, as everything here.
+ *
+ *   - Device pointers of the current HIP device; work is enqueued on
+ *     `hip_stream` (NULL = the default stream) and the call returns without
+ *     synchronising.  Kernel launches only: no allocation, no memset, so a call
+ *     may be captured into a HIP graph.
+ *   - Where an operator has a ..._workspace function, `workspace` is a device
+ *     buffer of at least that many bytes, 256-byte aligned (any allocation is),
+ *     which may be NULL where the function returns 0.  Its contents before the
+ *     call do not matter, nothing is kept in it between calls, and it may be
+ *     reused once the call's work has run: calls that overlap in time (two
+ *     streams, two graphs) need one each.
+ *   - Element types: fp32 or bf16 arrays as `dtype` says; everything named fp32
+ *     is fp32 whatever the dtype.  Arithmetic is in fp32 or wider.  Arrays are
+ *     aligned to their element; 16-byte aligned ones are faster.
+ *   - Results do not depend on what else runs: two calls on the same inputs give
+ *     the same bits.
+ *   - Errors as everywhere: SEED_ERR_INVALID_ARG for a null pointer or a size or
+ *     field out of range, SEED_ERR_ALIASING for outputs that overlap what they
+ *     must not, SEED_ERR_DEVICE if a launch fails.  Nothing has been enqueued
+ *     then.  seed_op_last_error returns the text of the last failed call of an
+ *     operator on the calling thread, never NULL.
+ * ------------------------------------------------------------------------ */
+enum { SEED_DTYPE_FP32 = 0, SEED_DTYPE_BF16 = 1 };
+enum { SEED_ACT_NONE = 0, SEED_ACT_RELU = 1, SEED_ACT_SILU = 2 };
+
+const char* seed_op_last_error(void);
+
+/*
+ * Linear attention with a decay for each head: a recurrent core whose state is
+ * a [key_dim, value_dim] matrix per row and head.  For step t of a row, head h:
+ *
+ *   S_t = decay[h] * S_{t-1} + k_t v_t^T       out_t = scale * q_t^T S_t
+ *
+ * S_{-1} is state_in.  Where done[t] is set S_{t-1} is taken as zero, as in
+ * seed_infer_unroll: an episode starts with step t, and nothing of what was
+ * before it is read into the state.  steps == 1 is the form for single tokens.
+ *
+ *   q      [steps, rows, heads, key_dim]      out  [steps, rows, heads, value_dim]
+ *   k, v   [steps, rows, kv_heads, key_dim] and [..., value_dim]; head h uses
+ *          key / value head h / (heads / kv_heads)
+ *          A row's heads are dense; steps and rows have strides of their own
+ *          (elements, not negative), so that the three may be parts of one
+ *          projection's output and the order may be time- or batch-major.
+ *   decay  [heads] fp32, usually in [0, 1]
+ *   done   [steps, rows] uint8, dense, or NULL
+ *   lengths [rows] int32 or NULL (all `steps`): row b has lengths[b] steps
+ *          (clamped to 0 .. steps); what lies behind them is neither read nor
+ *          written, and state_out is the state after the last of them
+ *   state_in  [rows, heads, key_dim, value_dim] fp32 or NULL (zero)
+ *   state_out the same shape; may be state_in itself, else must not overlap it
+ *
+ * out must not overlap q, k or v; state_out no other array.  1 <= key_dim,
+ * value_dim <= 256, kv_heads divides heads.  steps == 0 copies the state (zero
+ * where state_in is NULL); rows == 0 is a no-op.
+ * Products of bf16 inputs are exact and added in fp32; the state is fp32
+ * throughout.  A value that is not finite reaches the steps behind it, up to
+ * the next step whose done is set, and nothing else.
+ */
+typedef struct seed_decay {
+    uint32_t struct_size;                    /* = sizeof(seed_decay_t) */
+    int32_t dtype;                           /* of q, k, v and out */
+    int32_t steps, rows, heads, kv_heads, key_dim, value_dim;
+    float scale;
+    int64_t q_step, q_row, k_step, k_row, v_step, v_row, out_step, out_row;
+} seed_decay_t;
+
+size_t seed_op_decay_workspace(const seed_decay_t* desc);    /* 0 if desc is invalid */
+seed_status_t seed_op_decay(const seed_decay_t* desc, const void* q, const void* k, const void* v,
+                            const float* decay, const uint8_t* done, const int32_t* lengths,
+                            const float* state_in, void* out, float* state_out,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Group normalisation with an activation, channels last:
+ *
+ *   y = act((x - mean) / sqrt(var + eps) * weight + bias)
+ *
+ * mean and (population) variance over the points of a row and the channels of a
+ * group (channels / groups consecutive ones).  A row is a map of `points` =
+ * h * w pixels, or one vector (points = 1: a core's output head by head).
+ *
+ *   x, out   [rows, points, channels], dense; out may be x itself, else must
+ *            not overlap it
+ *   weight, bias   [channels] fp32, each may be NULL
+ *   activation     SEED_ACT_NONE, SEED_ACT_RELU or SEED_ACT_SILU (v * sigmoid(v))
+ *
+ * groups divides channels, eps >= 0.  rows == 0 or points == 0 is a no-op.
+ */
+size_t seed_op_group_norm_workspace(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups);
+seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups,
+                                 const void* x, const float* weight, const float* bias, float eps,
+                                 int32_t activation, void* out,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Sampling with temperature, top-k, top-p and min-p from one given uniform per
+ * row.  With m_j = exp((logit_j - max logit) / temperature) and the choices in
+ * the order (logit descending, index ascending), kept is the longest prefix of
+ * that order with
+ *   - at most top_k choices,
+ *   - in front of its last choice less than top_p of the top-k choices' mass,
+ *   - m_j >= min_p for every choice,
+ * and never fewer than one choice.  The result is the first choice of the order
+ * at which the running sum of m exceeds uniform * (the sum over the kept ones).
+ * Masses are computed and compared in 64 bits.
+ *
+ *   logits       [rows, choices], `row_stride` elements (not negative) between rows
+ *   uniforms     [rows] fp32 in [0, 1) (values outside are clamped, NaN is 0)
+ *   temperature  [rows] fp32 or NULL (1); <= 0 or NaN: the first of the order
+ *   top_k        [rows] int32 or NULL; <= 0 or >= choices: off
+ *   top_p        [rows] fp32 or NULL; >= 1 or NaN: off
+ *   min_p        [rows] fp32 or NULL; <= 0 or NaN: off
+ *   token_out    [rows] int32: the choice, -1 for a row without any
+ *   logprob_out  [rows] fp32: the log of its probability among the kept ones
+ *                (0 if greedy, -inf without a choice), or NULL
+ *
+ * A logit of -inf or NaN is no choice; equal logits of +inf share the mass.
+ * 1 <= choices <= SEED_SAMPLE_MAX_CHOICES; rows == 0 is a no-op.
+ */
+#define SEED_SAMPLE_MAX_CHOICES (1 << 24)
+size_t seed_op_sample_workspace(int32_t dtype, int32_t rows, int32_t choices);
+seed_status_t seed_op_sample(int32_t dtype, int32_t rows, int32_t choices, int64_t row_stride,
+                             const void* logits, const float* uniforms, const float* temperature,
+                             const int32_t* top_k, const float* top_p, const float* min_p,
+                             int32_t* token_out, float* logprob_out,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------
  * Diagnostics.  Not part of the inference path: a tap for tests that compare

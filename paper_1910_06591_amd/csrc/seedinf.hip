@@ -545,7 +545,9 @@ static seed_status_t step_impl(seed_infer_t* h, int32_t B, const uint8_t* obs,
         return fail(SEED_ERR_INVALID_ARG, "a recurrent arch needs prev_action, prev_reward, h_in, c_in, h_out and c_out");
     if (!rec && (prev_action || prev_reward || h_in || c_in || h_out || c_out))
         return fail(SEED_ERR_INVALID_ARG, "a feed-forward arch takes no recurrent arguments (pass NULL)");
-    if (a.select == SEED_SELECT_GUMBEL && !uniforms) return fail(SEED_ERR_INVALID_ARG, "Gumbel-max selection needs uniforms");
+    const bool sampled = ext && ext->struct_size == sizeof(seed_step_ext_t) && ext->sample_uniforms;
+    if (sampled && uniforms) return fail(SEED_ERR_INVALID_ARG, "a step with sample_uniforms takes no uniforms (pass NULL)");
+    if (!sampled && a.select == SEED_SELECT_GUMBEL && !uniforms) return fail(SEED_ERR_INVALID_ARG, "Gumbel-max selection needs uniforms");
     if (a.select == SEED_SELECT_GREEDY && uniforms) return fail(SEED_ERR_INVALID_ARG, "greedy selection takes no uniforms (pass NULL)");
     if (misaligned16(obs, h_in, c_in, h_out, c_out))
         return fail(SEED_ERR_INVALID_ARG, "obs, h_in, c_in, h_out and c_out must be 16-byte aligned");
@@ -553,10 +555,14 @@ static seed_status_t step_impl(seed_infer_t* h, int32_t B, const uint8_t* obs,
     const float* epsilon = nullptr;
     const float* explore_u = nullptr;
     if (ext) {
-        if (ext->struct_size != sizeof(seed_step_ext_t)) return fail(SEED_ERR_INVALID_ARG, "ext->struct_size is not sizeof(seed_step_ext_t)");
+        if (ext->struct_size != sizeof(seed_step_ext_t) && ext->struct_size != SEED_STEP_EXT_SIZE_EPISODE)
+            return fail(SEED_ERR_INVALID_ARG, "ext->struct_size is not sizeof(seed_step_ext_t)");
         done = ext->done; epsilon = ext->epsilon; explore_u = ext->explore_uniforms;
         if (done && !rec) return fail(SEED_ERR_INVALID_ARG, "done flags need a recurrent arch");
         if ((epsilon == nullptr) != (explore_u == nullptr)) return fail(SEED_ERR_INVALID_ARG, "epsilon and explore_uniforms must be given together");
+        if (sampled && epsilon) return fail(SEED_ERR_INVALID_ARG, "epsilon and sample_uniforms are two ways to select: give one");
+        if (ext->struct_size == sizeof(seed_step_ext_t) && !sampled && (ext->temperature || ext->top_k || ext->top_p || ext->min_p))
+            return fail(SEED_ERR_INVALID_ARG, "temperature, top_k, top_p and min_p need sample_uniforms");
     }
     if (rec) {
         size_t nb = (size_t)B * a.lstm_units * sizeof(float);
@@ -569,11 +575,19 @@ static seed_status_t step_impl(seed_infer_t* h, int32_t B, const uint8_t* obs,
     if (dev != h->device) return fail(SEED_ERR_INVALID_ARG, "current HIP device differs from the handle's device");
 
     hipStream_t s = (hipStream_t)hip_stream;
+    auto core_heads = [&]() -> seed_status_t {
+        seed_status_t st = run_core_heads(h, s, 0, B, prev_action, prev_reward, h_in, c_in, done, h_out, c_out, uniforms, epsilon, explore_u,
+                                          action_out, logits_out, value_out, probs_out);
+        if (st != SEED_OK || !sampled) return st;
+        // the heads left their greedy choice; the sampler's takes its place
+        st = seed_op_sample(SEED_DTYPE_FP32, B, a.num_actions, a.num_actions, logits_out, ext->sample_uniforms, ext->temperature, ext->top_k,
+                            ext->top_p, ext->min_p, action_out, nullptr, nullptr, 0, hip_stream);
+        if (st != SEED_OK) h->err = seed_op_last_error();
+        return st;
+    };
     if (!static_ws) {
         seed_status_t st = run_torso_fc(h, s, B, obs, arrival);
-        if (st != SEED_OK) return st;
-        return run_core_heads(h, s, 0, B, prev_action, prev_reward, h_in, c_in, done, h_out, c_out, uniforms, epsilon, explore_u,
-                              action_out, logits_out, value_out, probs_out);
+        return st == SEED_OK ? core_heads() : st;
     }
     // The same kernels on a workspace laid out in the static array.  Only host-side pointers change hands: the
     // kernels receive theirs by value at launch, and a handle is used from one thread at a time.
@@ -605,9 +619,7 @@ static seed_status_t step_impl(seed_infer_t* h, int32_t B, const uint8_t* obs,
     const WorkspacePtrs own = workspace_get(h);
     workspace_set(h, ws);
     seed_status_t st = run_torso_fc(h, s, B, obs);
-    if (st == SEED_OK)
-        st = run_core_heads(h, s, 0, B, prev_action, prev_reward, h_in, c_in, done, h_out, c_out, uniforms, epsilon, explore_u,
-                            action_out, logits_out, value_out, probs_out);
+    if (st == SEED_OK) st = core_heads();
     workspace_set(h, own);
     return st;
 }

@@ -18,6 +18,7 @@ LIB_PATH = os.environ.get("SEEDINF_LIB", os.path.join(_PKG, "libseedinf.so"))
 SOURCES = [os.path.join(_PKG, "csrc", f) for f in
            ("seedinf.hip", "plan.h", "kernels_fp32.h", "kernels_heads.h", "bf16_path.h", "bf16_common.h", "gemm_bf16.h", "gemm_bf16_lds.h",
             "conv_stack_bf16.h", "conv_stack_fused.h", "resnet_fused.h", "resnet_layerwise.h", "resnet_blockfused.h", "resnet_firstpool.h", "resnet_convpool.h", "resnet_convtile.h", "resnet_strip.h", "resnet_pair.h", "resnet_rows.h", "batcher.h", "host_pool.h")]
+OP_SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("ops.hip", "op_common.h", "op_decay.h", "op_norm.h", "op_sample.h")]
 PROBE_SOURCE = os.path.join(_PKG, "csrc", "probe.hip")
 PROBE_LIB_PATH = os.path.join(_PKG, "libseedprobe.so")
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -32,12 +33,24 @@ EXPORTS = ["seed_infer_weight_count", "seed_infer_validate", "seed_infer_create"
            "seed_batcher_read_state", "seed_batcher_stream", "seed_batcher_last_error", "seed_batcher_destroy",
            "seed_infer_read_intermediate", "seed_infer_torso_features", "seed_infer_last_error",
            "seed_infer_destroy", "seed_infer_set_profiling", "seed_infer_profile_read"]
+OP_EXPORTS = ["seed_op_last_error", "seed_op_decay_workspace", "seed_op_decay", "seed_op_group_norm_workspace", "seed_op_group_norm",
+              "seed_op_sample_workspace", "seed_op_sample"]
 
 
 class SeedStepExt(C.Structure):
     """seed_step_ext_t: optional inputs of seed_infer_step_ext (device pointers, 0 = absent)."""
     _fields_ = [("struct_size", C.c_uint32), ("done", C.c_void_p), ("epsilon", C.c_void_p),
-                ("explore_uniforms", C.c_void_p)]
+                ("explore_uniforms", C.c_void_p), ("sample_uniforms", C.c_void_p), ("temperature", C.c_void_p),
+                ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
+class SeedDecay(C.Structure):
+    """seed_decay_t: sizes and strides of one seed_op_decay call."""
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32),
+                ("steps", C.c_int32), ("rows", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("key_dim", C.c_int32), ("value_dim", C.c_int32), ("scale", C.c_float),
+                ("q_step", C.c_int64), ("q_row", C.c_int64), ("k_step", C.c_int64), ("k_row", C.c_int64),
+                ("v_step", C.c_int64), ("v_row", C.c_int64), ("out_step", C.c_int64), ("out_row", C.c_int64)]
 
 
 class SeedError(RuntimeError):
@@ -65,8 +78,8 @@ class SeedArch(C.Structure):
 def build_library(verbose: bool = False) -> str:
     """Compile csrc/ into libseedinf.so (and the measurement probes into
     libseedprobe.so) for gfx950 with hipcc (cross-compiles without a GPU)."""
-    for src, out in ((SOURCES[0], LIB_PATH), (PROBE_SOURCE, PROBE_LIB_PATH)):
-        cmd = ["hipcc", *HIPCC_FLAGS, src, "-o", out]
+    for srcs, out in (((SOURCES[0], OP_SOURCES[0]), LIB_PATH), ((PROBE_SOURCE,), PROBE_LIB_PATH)):
+        cmd = ["hipcc", *HIPCC_FLAGS, *srcs, "-o", out]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + r.stderr)
@@ -150,6 +163,20 @@ def load_library():
     lib.seed_infer_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32)]
     lib.seed_infer_destroy.restype = None
     lib.seed_infer_destroy.argtypes = [C.c_void_p]
+    lib.seed_op_last_error.restype = C.c_char_p
+    lib.seed_op_last_error.argtypes = []
+    lib.seed_op_decay_workspace.restype = C.c_size_t
+    lib.seed_op_decay_workspace.argtypes = [C.c_void_p]
+    lib.seed_op_decay.restype = C.c_int
+    lib.seed_op_decay.argtypes = [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]
+    lib.seed_op_group_norm_workspace.restype = C.c_size_t
+    lib.seed_op_group_norm_workspace.argtypes = [C.c_int32] * 5
+    lib.seed_op_group_norm.restype = C.c_int
+    lib.seed_op_group_norm.argtypes = [C.c_int32] * 5 + [C.c_void_p] * 3 + [C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.seed_op_sample_workspace.restype = C.c_size_t
+    lib.seed_op_sample_workspace.argtypes = [C.c_int32] * 3
+    lib.seed_op_sample.restype = C.c_int
+    lib.seed_op_sample.argtypes = [C.c_int32] * 3 + [C.c_int64] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 
@@ -257,12 +284,14 @@ class SeedInfer:
 
     def step(self, obs, prev_action=None, prev_reward=None, h_in=None, c_in=None, uniforms=None,
              want_probs=True, out=None, stream=None, done=None, epsilon=None, explore_uniforms=None,
-             static_workspace=False):
+             static_workspace=False, sample_uniforms=None, temperature=None, top_k=None, top_p=None, min_p=None):
         """Run one inference step on device tensors; returns a dict of device
         tensors (allocated here with torch unless `out` supplies them).  done [B] uint8,
         epsilon [B] and explore_uniforms [B, 2] are the optional episode flags and
-        epsilon-greedy inputs (seed_infer_step_ext).  static_workspace=True calls
-        seed_infer_step_static (the library's static device workspace) instead."""
+        epsilon-greedy inputs, sample_uniforms [B] with temperature, top_k (int32),
+        top_p and min_p [B] those of filtered sampling (seed_infer_step_ext).
+        static_workspace=True calls seed_infer_step_static (the library's static
+        device workspace) instead."""
         import torch
         a = self.arch
         B = obs.shape[0]
@@ -278,12 +307,17 @@ class SeedInfer:
                 out["probs"] = torch.empty(B, self.A, dtype=torch.float32, device=dev)
         s = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
         ext = None
-        if done is not None or epsilon is not None or explore_uniforms is not None:
+        if any(x is not None for x in (done, epsilon, explore_uniforms, sample_uniforms, temperature, top_k, top_p, min_p)):
             addr = lambda p_: None if p_ is None else p_.value
             ext = SeedStepExt(C.sizeof(SeedStepExt),
                               addr(_ptr(done, torch.uint8, (B,), "done")),
                               addr(_ptr(epsilon, torch.float32, (B,), "epsilon")),
-                              addr(_ptr(explore_uniforms, torch.float32, (B, 2), "explore_uniforms")))
+                              addr(_ptr(explore_uniforms, torch.float32, (B, 2), "explore_uniforms")),
+                              addr(_ptr(sample_uniforms, torch.float32, (B,), "sample_uniforms")),
+                              addr(_ptr(temperature, torch.float32, (B,), "temperature")),
+                              addr(_ptr(top_k, torch.int32, (B,), "top_k")),
+                              addr(_ptr(top_p, torch.float32, (B,), "top_p")),
+                              addr(_ptr(min_p, torch.float32, (B,), "min_p")))
         entry = self.lib.seed_infer_step_static if static_workspace else self.lib.seed_infer_step_ext
         st = entry(
             self._h, B,
@@ -451,3 +485,181 @@ class Batcher:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------- stand-alone operators (seed_op_*)
+
+_ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+
+
+def _op_dtype(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _op_arg(t, dtype, shape, name, device):
+    """Address of a contiguous tensor on `device`, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous {dtype} of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class _OpCall:
+    """The device and stream of one operator call.  Memory allocated inside belongs to that stream: a workspace goes
+    back to torch's allocator behind the kernels that use it, whichever stream that is."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.device, self.stream = device, stream
+        self.guards = []
+        if device.index != torch.cuda.current_device():
+            self.guards.append(torch.cuda.device(device))
+        if stream is not None:
+            self.guards.append(torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)))
+
+    def __enter__(self):
+        import torch
+        for g in self.guards:
+            g.__enter__()
+        if self.stream is None:
+            self.stream = torch.cuda.current_stream(self.device).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+    def workspace(self, n):
+        import torch
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+
+def _op_check(lib, st):
+    if st != 0:
+        raise SeedError(st, lib.seed_op_last_error().decode())
+
+
+def _strided(t, shape, name, dtype, device):
+    """A [steps, rows, heads, dim] tensor whose heads are dense in a row: its address and the strides of a step and a row."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
+        raise TypeError(f"{name} must be {dtype} of shape {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    st = t.stride()
+    if t.numel() and ((shape[3] > 1 and st[3] != 1) or (shape[2] > 1 and st[2] != shape[3])):
+        raise TypeError(f"{name}: a row's heads must be dense, got strides {st}")
+    return t.data_ptr(), st[0], st[1]
+
+
+def decay_attention(q, k, v, decay, state=None, done=None, lengths=None, scale=1.0, out=None, state_out=None, stream=None):
+    """Linear attention with a decay for each head (seed_op_decay) over a time axis:
+    S_t = decay S_{t-1} + k_t v_t^T (S_{t-1} = 0 where done_t is set), out_t = scale q_t^T S_t.
+
+    q [steps, rows, heads, key_dim], k and v [steps, rows, kv_heads, key_dim / value_dim], fp32 or bf16, any strides of
+    steps and rows; decay [heads] fp32; state [rows, heads, key_dim, value_dim] fp32 or None (zero); done [steps, rows]
+    uint8; lengths [rows] int32: the steps behind a row's length are neither read nor written (`out` is zero there where
+    it is allocated here).  Returns out [steps, rows, heads, value_dim] and the state after the last step; `state_out`
+    may be `state` itself."""
+    import torch
+    lib = load_library()
+    dt, dev, dtype = _op_dtype(q, "q"), q.device, q.dtype
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise TypeError("q, k and v must be [steps, rows, heads, dim]")
+    T, B, H, dk = q.shape
+    KV, dv = k.shape[2], v.shape[3]
+    with _OpCall(dev, stream) as call:
+        if out is None:
+            out = (torch.empty if lengths is None else torch.zeros)((T, B, H, dv), dtype=dtype, device=dev)
+        if state_out is None:
+            state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev)
+        pq, q0, q1 = _strided(q, (T, B, H, dk), "q", dtype, dev)
+        pk, k0, k1 = _strided(k, (T, B, KV, dk), "k", dtype, dev)
+        pv, v0, v1 = _strided(v, (T, B, KV, dv), "v", dtype, dev)
+        po, o0, o1 = _strided(out, (T, B, H, dv), "out", dtype, dev)
+        d = SeedDecay(C.sizeof(SeedDecay), dt, T, B, H, KV, dk, dv, scale, q0, q1, k0, k1, v0, v1, o0, o1)
+        ref = C.byref(d)
+        need = lib.seed_op_decay_workspace(ref)
+        ws = call.workspace(need)
+        _op_check(lib, lib.seed_op_decay(
+            ref, pq, pk, pv, _op_arg(decay, torch.float32, (H,), "decay", dev), _op_arg(done, torch.uint8, (T, B), "done", dev),
+            _op_arg(lengths, torch.int32, (B,), "lengths", dev), _op_arg(state, torch.float32, (B, H, dk, dv), "state", dev), po,
+            _op_arg(state_out, torch.float32, (B, H, dk, dv), "state_out", dev), None if ws is None else ws.data_ptr(), need, call.stream))
+    return out, state_out
+
+
+def decay_step(q, k, v, decay, state=None, done=None, scale=1.0, out=None, state_out=None, stream=None):
+    """decay_attention for single tokens: q [rows, heads, key_dim], k, v [rows, kv_heads, ...], done [rows], out
+    [rows, heads, value_dim]."""
+    out, state_out = decay_attention(q[None], k[None], v[None], decay, state, None if done is None else done[None], None, scale,
+                                     None if out is None else out[None], state_out, stream)
+    return out[0], state_out
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", out=None, stream=None):
+    """Group normalisation with an activation ("none", "relu", "silu"), channels last (seed_op_group_norm): x [rows, ...,
+    channels] contiguous, fp32 or bf16; weight and bias [channels] fp32.  `out` may be x itself."""
+    import torch
+    lib = load_library()
+    dt, dev = _op_dtype(x, "x"), x.device
+    if x.dim() < 2:
+        raise TypeError("x must be [rows, ..., channels]")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
+    N, Cn = x.shape[0], x.shape[-1]
+    P = 1
+    for n in x.shape[1:-1]:
+        P *= n
+    with _OpCall(dev, stream) as call:
+        if out is None:
+            out = torch.empty_like(x)
+        need = lib.seed_op_group_norm_workspace(dt, N, P, Cn, groups)
+        ws = call.workspace(need)
+        _op_check(lib, lib.seed_op_group_norm(
+            dt, N, P, Cn, groups, _op_arg(x, x.dtype, x.shape, "x", dev), _op_arg(weight, torch.float32, (Cn,), "weight", dev),
+            _op_arg(bias, torch.float32, (Cn,), "bias", dev), eps, _ACTIVATIONS[activation], _op_arg(out, x.dtype, x.shape, "out", dev),
+            None if ws is None else ws.data_ptr(), need, call.stream))
+    return out
+
+
+def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, stream=None):
+    """Sampling with temperature, top-k, top-p and min-p from one given uniform a row (seed_op_sample): logits [rows,
+    choices] fp32 or bf16 with dense rows, uniforms [rows]; temperature, top_p, min_p [rows] fp32 and top_k [rows] int32,
+    each optional, a number standing for that value in every row.  Returns token [rows] int32 and its log-probability
+    among the kept choices [rows] fp32."""
+    import torch
+    lib = load_library()
+    dt, dev = _op_dtype(logits, "logits"), logits.device
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError("logits must be [rows, choices] with dense rows")
+    R, V = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    with _OpCall(dev, stream) as call:
+        if token is None:
+            token = torch.empty(R, dtype=i32, device=dev)
+        if logprob is None:
+            logprob = torch.empty(R, dtype=f32, device=dev)
+
+        keep = []
+
+        def per_row(x, dtype, name):
+            if x is None:
+                return None
+            if not isinstance(x, torch.Tensor):
+                x = torch.full((R,), x, dtype=dtype, device=dev)
+                keep.append(x)
+            return _op_arg(x, dtype, (R,), name, dev)
+
+        need = lib.seed_op_sample_workspace(dt, R, V)
+        ws = call.workspace(need)
+        _op_check(lib, lib.seed_op_sample(
+            dt, R, V, logits.stride(0), logits.data_ptr(), _op_arg(uniforms, f32, (R,), "uniforms", dev),
+            per_row(temperature, f32, "temperature"), per_row(top_k, i32, "top_k"), per_row(top_p, f32, "top_p"), per_row(min_p, f32, "min_p"),
+            _op_arg(token, i32, (R,), "token", dev), _op_arg(logprob, f32, (R,), "logprob", dev),
+            None if ws is None else ws.data_ptr(), need, call.stream))
+    return token, logprob

@@ -1,0 +1,248 @@
+"""seed_op_decay on the GPU against the recurrence in 64 bits: sizes from one step and one unit up, odd sizes, shared key
+and value heads, episode flags, rows of unequal length, strides, and what must not be read or written."""
+import numpy as np
+import pytest
+
+from paper_1910_06591_amd import seedinf
+from tests import ops_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def make(T, B, H, KV, dk, dv, dtype, seed=0, done=0.0, lengths=None, state=True, decay=None):
+    import torch
+    rng = np.random.default_rng(seed)
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    x = {n: torch.from_numpy(rng.standard_normal(s).astype(np.float32) * f).cuda().to(dt)
+         for n, s, f in (("q", (T, B, H, dk), 1.0), ("k", (T, B, KV, dk), dk ** -0.5), ("v", (T, B, KV, dv), 1.0))}
+    g = rng.uniform(0.5, 0.999, H).astype(np.float32) if decay is None else np.resize(np.float32(decay), H)
+    x["decay"] = torch.from_numpy(g).cuda()
+    x["state"] = torch.from_numpy(rng.standard_normal((B, H, dk, dv)).astype(np.float32)).cuda() if state else None
+    x["done"] = torch.from_numpy((rng.random((T, B)) < done).astype(np.uint8)).cuda() if done else None
+    x["lengths"] = torch.tensor(lengths, dtype=torch.int32).cuda() if lengths is not None else None
+    return x
+
+
+def host(x):
+    return None if x is None else x.double().cpu().numpy()
+
+
+def check(x, out, state, scale, bf16):
+    ro, rs, mag, A = ref.decay(host(x["q"]), host(x["k"]), host(x["v"]), host(x["decay"]), host(x["state"]), host(x["done"]),
+                               None if x["lengths"] is None else x["lengths"].cpu().numpy(), scale)
+    tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, x["q"].shape[0], x["q"].shape[3], bf16)
+    there = ~np.isnan(ro)
+    eo, es = np.abs(host(out) - ro)[there], np.abs(host(state) - rs)
+    assert np.isfinite(host(out)[there]).all() and np.isfinite(host(state)).all()
+    assert (eo <= tol_o[there]).all(), f"out: worst {np.max(eo / tol_o[there]):.2f} of the tolerance"
+    assert (es <= tol_s).all(), f"state: worst {np.max(es / tol_s):.2f} of the tolerance"
+
+
+SIZES = [  # T, B, H, KV, dk, dv
+    (1, 1, 1, 1, 1, 1), (1, 3, 4, 4, 64, 64), (1, 5, 2, 1, 33, 17), (1, 4, 8, 2, 128, 128), (1, 2, 1, 1, 256, 256), (1, 300, 3, 3, 20, 70),
+    (2, 2, 2, 2, 64, 64), (7, 3, 4, 2, 16, 100), (31, 2, 2, 1, 64, 64), (32, 5, 4, 4, 64, 64), (33, 2, 2, 2, 128, 128), (63, 1, 2, 2, 100, 36),
+    (64, 1, 1, 1, 64, 128), (65, 2, 4, 1, 128, 64), (130, 1, 3, 3, 7, 9), (129, 2, 1, 1, 256, 65), (200, 2, 2, 2, 130, 256), (1000, 1, 2, 2, 64, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,H,KV,dk,dv", SIZES)
+def test_sizes(T, B, H, KV, dk, dv, dtype):
+    x = make(T, B, H, KV, dk, dv, dtype, seed=T + dk)
+    out, state = seedinf.decay_attention(**x, scale=0.7)
+    check(x, out, state, 0.7, dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,done", [(1, 40, 0.5), (9, 6, 0.3), (70, 4, 0.05), (200, 3, 0.02), (150, 2, 1.0)])
+def test_episode_flags(T, B, done, dtype):
+    """A flagged row starts from zero; the state in front of it is not read (it is NaN where the first step is flagged)."""
+    x = make(T, B, 2, 2, 64, 48, dtype, seed=T, done=done)
+    flagged = x["done"][0] != 0
+    ok = dict(x, state=x["state"].clone())
+    ok["state"][flagged] = 0
+    x["state"][flagged] = float("nan")
+    out, state = seedinf.decay_attention(**x)
+    check(ok, out, state, 1.0, dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [5, 40, 140, 700])
+def test_lengths(T, dtype):
+    """Steps behind a row's length: inputs (NaN here) are not read, outputs stay as they were, the state is the one at the length."""
+    lengths = [T, 0, 1, T - 1, T // 2, T + 9, -3]
+    x = make(T, len(lengths), 2, 1, 64, 64, dtype, seed=T, done=0.1, lengths=lengths)
+    import torch
+    out = torch.full((T, len(lengths), 2, 64), 7.0, dtype=x["q"].dtype, device="cuda")
+    poisoned = {n: x[n].clone() for n in "qkv"}
+    for b, n in enumerate(lengths):
+        for name in "qkv":
+            poisoned[name][max(0, min(n, T)):, b] = float("nan")
+    got, state = seedinf.decay_attention(**dict(x, **poisoned), out=out)
+    for b, n in enumerate(lengths):
+        assert (got[max(0, min(n, T)):, b] == 7.0).all()
+    check(x, got, state, 1.0, dtype == "bf16")
+    zeros, _ = seedinf.decay_attention(**dict(x, **poisoned))
+    assert (zeros[1:, 2] == 0).all()
+
+
+@pytest.mark.parametrize("decay", [[0.0], [1.0], [1e-30, 0.99999, 0.5]])
+@pytest.mark.parametrize("T", [1, 20, 150])
+def test_extreme_decays(T, decay):
+    x = make(T, 2, 3, 3, 64, 64, "fp32", seed=3, decay=decay)
+    out, state = seedinf.decay_attention(**x)
+    check(x, out, state, 1.0, False)
+
+
+def test_no_state_given_and_no_steps():
+    import torch
+    x = make(80, 2, 2, 2, 64, 64, "bf16", state=False)
+    out, state = seedinf.decay_attention(**x)
+    check(x, out, state, 1.0, True)
+    y = make(0, 3, 2, 2, 64, 64, "bf16")
+    out, state = seedinf.decay_attention(**y)
+    assert out.shape == (0, 3, 2, 64) and torch.equal(state, y["state"])
+    _, state = seedinf.decay_attention(**dict(y, state=None))
+    assert (state == 0).all()
+    out, state = seedinf.decay_attention(**make(4, 0, 2, 2, 64, 64, "bf16"))
+    assert out.numel() == 0 and state.numel() == 0
+
+
+@pytest.mark.parametrize("T", [6, 100, 900])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_strides_and_orders(T, dtype):
+    """Parts of one projection's output, batch-major arrays, arrays at odd addresses: the same bits as dense ones."""
+    import torch
+    B, H, dk, dv = 3, 2, 64, 32
+    x = make(T, B, H, H, dk, dv, dtype, seed=T)
+    out, state = seedinf.decay_attention(**x)
+    row = torch.cat([x["q"].flatten(2), x["k"].flatten(2), x["v"].flatten(2), torch.zeros_like(x["v"].flatten(2))], 2)
+    a, b, c = H * dk, 2 * H * dk, 2 * H * dk + H * dv
+    part = lambda lo, hi, d: row[:, :, lo:hi].view(T, B, H, d)  # noqa: E731
+    o2, s2 = seedinf.decay_attention(part(0, a, dk), part(a, b, dk), part(b, c, dv), x["decay"], state=x["state"], out=part(c, c + H * dv, dv))
+    assert torch.equal(out, o2) and torch.equal(state, s2) and torch.equal(row[:, :, :a], x["q"].flatten(2))
+    swap = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    o3, s3 = seedinf.decay_attention(swap(x["q"]), swap(x["k"]), swap(x["v"]), x["decay"], state=x["state"], out=swap(torch.zeros_like(out)))
+    assert torch.equal(out, o3) and torch.equal(state, s3)
+
+    def odd(t):
+        flat = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:]
+        return flat.copy_(t.flatten()).view(t.shape)
+    o4, s4 = seedinf.decay_attention(odd(x["q"]), odd(x["k"]), odd(x["v"]), x["decay"], state=odd(x["state"]), out=odd(out), state_out=odd(state))
+    assert torch.equal(out, o4) and torch.equal(state, s4)
+
+
+@pytest.mark.parametrize("T", [1, 12, 100, 2000])
+def test_state_in_place_and_handed_over(T):
+    """state_out may be state; a sequence in two calls is the sequence in one, up to rounding."""
+    import torch
+    x = make(T, 2, 4, 2, 128, 128, "bf16", seed=5)
+    out, state = seedinf.decay_attention(**x)
+    s = x["state"].clone()
+    o2, s2 = seedinf.decay_attention(**dict(x, state=s), state_out=s)
+    assert s2 is s and torch.equal(out, o2) and torch.equal(state, s)
+    cut = T // 3
+    first = {n: x[n][:cut] for n in "qkv"}
+    rest = {n: x[n][cut:] for n in "qkv"}
+    oa, sa = seedinf.decay_attention(**dict(x, **first))
+    ob, sb = seedinf.decay_attention(**dict(x, **rest, state=sa))
+    check(x, torch.cat([oa, ob]), sb, 1.0, True)
+
+
+@pytest.mark.parametrize("T", [9, 90, 600])
+def test_values_that_are_not_finite_stay_in_their_episode(T):
+    """An infinite key or a NaN value reaches the later steps of its episode only: not the steps before it, not the
+    episode behind the next flag, not the state after that, and no other row or head."""
+    import torch
+    x = make(T, 3, 2, 2, 64, 64, "bf16", seed=8)
+    done = torch.zeros(T, 3, dtype=torch.uint8, device="cuda")
+    bad, end = T // 3, T // 2
+    done[end, 1] = 1
+    x["done"] = done
+    y = dict(x, k=x["k"].clone(), v=x["v"].clone())
+    y["v"][bad, 1, 0, 3] = float("nan")
+    y["k"][bad, 1, 1, 5] = float("inf")
+    out, state = seedinf.decay_attention(**y)
+    clean = {n: x[n].clone() for n in "kv"}
+    clean["k"][bad:end, 1], clean["v"][bad:end, 1] = 0, 0           # (the reference's own sums stay finite)
+    keep = torch.ones(T, 3, dtype=torch.bool, device="cuda")
+    keep[bad:end, 1] = False
+    want, _ = seedinf.decay_attention(**dict(x, **clean))
+    assert torch.isfinite(out[keep]).all() and torch.isfinite(state).all()
+    assert not torch.isfinite(out[bad:end, 1, 0, 3]).any()
+    ro, rs, mag, A = ref.decay(*(host(z) for z in (x["q"], clean["k"], clean["v"], x["decay"], x["state"], done)))
+    tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, T, 64, True)
+    m = keep.cpu().numpy()
+    assert (np.abs(host(out) - ro)[m] <= tol_o[m]).all() and (np.abs(host(state) - rs) <= tol_s).all()
+
+
+def test_offsets_past_32_bits():
+    """A batch-major cache of sequences whose rows are further apart than 2^32 bytes."""
+    import torch
+    T, B, H, d = 70, 2, 2, 64
+    x = make(T, B, H, H, d, d, "bf16", seed=4)
+    far = 2 ** 31 + 4096                                              # elements between rows: more than 2^32 bytes
+    big = torch.empty(far + 4 * T * H * d, dtype=torch.bfloat16, device="cuda")
+
+    def place(t, at):
+        view = big.as_strided((T, B, H, d), (H * d, far, d, 1), at)
+        return view.copy_(t)
+    n = T * H * d
+    q, k, v = place(x["q"], 0), place(x["k"], n), place(x["v"], 2 * n)
+    out = big.as_strided((T, B, H, d), (H * d, far, d, 1), 3 * n)
+    want, s = seedinf.decay_attention(**x)
+    got, s2 = seedinf.decay_attention(q, k, v, x["decay"], state=x["state"], out=out)
+    assert torch.equal(want, got) and torch.equal(s, s2)
+
+
+def test_step_form_is_the_unroll_step_by_step():
+    import torch
+    T, B = 6, 5
+    x = make(T, B, 4, 2, 64, 64, "fp32", seed=2, done=0.2)
+    outs, s = [], x["state"]
+    for t in range(T):
+        o, s = seedinf.decay_step(x["q"][t], x["k"][t], x["v"][t], x["decay"], state=s, done=x["done"][t])
+        outs.append(o)
+    check(x, torch.stack(outs), s, 1.0, False)
+
+
+def test_graphs_and_streams():
+    """Captured and replayed with eager calls between, and on a stream that is not the current one."""
+    import torch
+    xs = [make(300, 2, 2, 2, 64, 64, "bf16", seed=s, done=0.02) for s in range(3)]
+    want = [seedinf.decay_attention(**x) for x in xs]
+    x = {k: None if v is None else v.clone() for k, v in xs[0].items()}
+    out, state = torch.zeros_like(want[0][0]), torch.zeros_like(want[0][1])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        seedinf.decay_attention(**x, out=out, state_out=state)
+    for r in range(5):
+        for k, v in xs[r % 3].items():
+            if v is not None:
+                x[k].copy_(v)
+        g.replay()
+        eager = seedinf.decay_attention(**xs[(r + 1) % 3])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[r % 3][0]) and torch.equal(state, want[r % 3][1]), r
+        assert torch.equal(eager[0], want[(r + 1) % 3][0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [seedinf.decay_attention(**y, stream=side.cuda_stream) for y in xs]
+    here = [seedinf.decay_attention(**y) for y in xs]
+    torch.cuda.synchronize()
+    for a, b, c in zip(got, here, want):
+        assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1]) and torch.equal(b[0], c[0])
+
+
+def test_binding_refuses():
+    x = make(4, 2, 4, 2, 16, 16, "bf16")
+    for bad in (dict(x, k=x["k"].float()), dict(x, k=x["k"][:3]), dict(x, q=x["q"][..., ::2]), dict(x, state=x["state"].bfloat16()),
+                dict(x, decay=x["decay"][:3]), dict(x, v=x["v"].cpu()), dict(x, q=x["q"].double())):
+        with pytest.raises(TypeError):
+            seedinf.decay_attention(**bad)
+    with pytest.raises(seedinf.SeedError):
+        seedinf.decay_attention(**dict(x, q=x["q"][:, :, :3].contiguous(), decay=x["decay"][:3].contiguous(), state=None))
+    with pytest.raises(seedinf.SeedError) as e:
+        seedinf.decay_attention(**x, out=x["q"])
+    assert e.value.status == seedinf.STATUS_BY_NAME["SEED_ERR_ALIASING"]
