@@ -14,7 +14,8 @@ template <class T> struct ElemVec;
 template <> struct ElemVec<float> { static constexpr int N = 4; typedef floatx4 V; };
 template <> struct ElemVec<__bf16> { static constexpr int N = 8; typedef bf16x8 V; };
 
-__device__ __forceinline__ float op_silu(float x) { return x / (1.0f + __expf(-x)); }
+// x / (1 + exp(-x)); the reciprocal instruction is good to one unit in the last place
+__device__ __forceinline__ float op_silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
 template <int ACT>
 __device__ __forceinline__ float op_activate(float x)

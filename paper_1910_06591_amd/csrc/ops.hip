@@ -153,8 +153,15 @@ static seed_status_t norm_check(int32_t dtype, int32_t rows, int32_t points, int
 
 extern "C" size_t seed_op_group_norm_workspace(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups)
 {
-    if (norm_check(dtype, rows, points, channels, groups) != SEED_OK) return 0;
-    return 0;
+    if (norm_check(dtype, rows, points, channels, groups) != SEED_OK || rows == 0 || points == 0) return 0;
+    // whatever the arrays' alignment turns out to be
+    size_t most = 0;
+    const int size = (int)op_dtype_size(dtype);
+    for (int vec = 16 / size; vec >= 1; vec /= 2) {
+        const size_t n = norm_plan(rows, points, channels, groups, size, vec).workspace;
+        if (n > most) most = n;
+    }
+    return most;
 }
 
 extern "C" seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups, const void* x,
@@ -174,9 +181,12 @@ extern "C" seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t
     if ((x != out && op_overlap(x, bytes, out, bytes)) || op_overlap(weight, (size_t)channels * 4, out, bytes) || op_overlap(bias, (size_t)channels * 4, out, bytes))
         return op_fail(SEED_ERR_ALIASING, "out overlaps x without being it, or weight or bias");
     if ((st = op_check_workspace(seed_op_group_norm_workspace(dtype, rows, points, channels, groups), workspace, workspace_bytes)) != SEED_OK) return st;
-    NormArgs p{x, out, weight, bias, rows, points, channels, groups, eps};
-    if (dtype == SEED_DTYPE_FP32) norm_launch<float>(p, activation, (hipStream_t)hip_stream);
-    else norm_launch<__bf16>(p, activation, (hipStream_t)hip_stream);
+    int vec = (int)(16 / size);
+    while (!op_aligned(x, vec * size) || !op_aligned(out, vec * size)) vec /= 2;
+    const NormPlan plan = norm_plan(rows, points, channels, groups, (int)size, vec);
+    NormArgs p{x, out, weight, bias, rows, points, channels, groups, eps, activation, op_aligned(weight, 16) && op_aligned(bias, 16)};
+    if (dtype == SEED_DTYPE_FP32) norm_launch<float>(p, plan, workspace, (hipStream_t)hip_stream);
+    else norm_launch<__bf16>(p, plan, workspace, (hipStream_t)hip_stream);
     return op_launched();
 }
 
