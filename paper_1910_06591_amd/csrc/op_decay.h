@@ -1,6 +1,8 @@
 // Linear attention with a decay for each head: a recurrent core whose state is a matrix per head,
 //   S_t = g S_{t-1} + k_t v_t^T   (S_{t-1} taken as zero where done_t is set),    o_t = scale q_t^T S_t.
 #pragma once
+#include <type_traits>
+
 #include "op_common.h"
 
 namespace seedinf {
@@ -17,6 +19,11 @@ struct DecayArgs {
     int T, B, H, KV, dk, dv;
     float scale;
     int vec_state;               // dv and the states' addresses allow 16-byte accesses
+    int vec_q, vec_k, vec_v;     // every step's heads are 16-byte aligned, dims whole vectors
+    int vec_o;                   // four outputs can be stored at once
+    int segments, segment_steps; // the time axis in parts that are worked on side by side; 1: not split
+    float* seg_state;            // [rows, heads, segments, dk, dv]: what a segment adds to the state, then the state in front of it
+    float2* seg_factor;          // [rows, heads, segments]: (power of the decay over the segment, 1 if a flag lies in it)
 };
 
 __device__ __forceinline__ int decay_length(const DecayArgs& p, int b)
@@ -107,13 +114,542 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
     }
 }
 
-template <class T>
-static void decay_launch(const DecayArgs& p, hipStream_t s)
+// ---- chunks: matrix products over 64 steps (bf16) or 32 (fp32) ----
+//
+// With S the state in front of a chunk, steps i, j counted inside it, and no flags,
+//   o_i = scale (g^(i+1) q_i^T S + sum_{j <= i} g^(i-j) (q_i . k_j) v_j),   S' = g^c S + sum_j g^(c-1-j) k_j v_j^T,
+// four products on the matrix units: scores, scores x values, queries x state, keys^T x values.  A flag at step r cuts
+// every power that spans it: j >= r where i >= r, and S takes no part from r on.  Powers are a table (in 64 bits, by
+// squaring: no logarithm of a decay of 0 or 1), never negative: nothing overflows where a decay is small.
+//
+// A workgroup (4 wavefronts) owns up to 128 columns of a head's state, each wavefront a quarter of the columns and all
+// rows, in accumulator registers for the whole time axis: S never travels through LDS.  The rows of the accumulator
+// tiles are the state's in an order (decay_row) in which a lane's values of two tiles are the eight consecutive key
+// elements that a bf16 operand wants, so S is an operand as it stands.
+//
+// Roundings: bf16 inputs are operands as they are.  What is computed between the products is split into bf16 parts whose
+// sum it is: scores and state into two (2^-16 of the value is lost, small beside the output's own 2^-8), the weighted
+// values of the state's update into three (nothing is lost: the state is fp32).  fp32 inputs use the fp32 matrix
+// instructions.
+//
+// A chunk with a value that is not finite is worked on step by step (chunks of one): a product with a zero weight
+// would carry it into steps before it and past flags.
+
+template <class T> struct DecayMma;
+template <> struct DecayMma<float> {
+    static constexpr int C = 32, FE = 4, KS = 16;           // steps a chunk; elements of an operand a lane; depth of a product
+    typedef floatx4 Frag;
+    static __device__ __forceinline__ floatx4 mma(floatx4 a, floatx4 b, floatx4 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct DecayMma<__bf16> {
+    static constexpr int C = 64, FE = 8, KS = 32;
+    typedef bf16x8 Frag;
+    static __device__ __forceinline__ floatx4 mma(bf16x8 a, bf16x8 b, floatx4 c) { return mfma16(a, b, c); }
+};
+
+// the state's row that row m of accumulator tile t holds
+template <class T> __device__ __forceinline__ int decay_row(int t, int m)
 {
+    if constexpr (sizeof(T) == 4) return 16 * t + m;
+    else return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3);
+}
+
+__device__ __forceinline__ bf16x8 decay_round8(const float (&x)[8]) { return to_bf16x8(floatx4{x[0], x[1], x[2], x[3]}, floatx4{x[4], x[5], x[6], x[7]}); }
+// x = hi + rest: rest in place of x
+__device__ __forceinline__ bf16x8 decay_split8(float (&x)[8])
+{
+    const bf16x8 hi = decay_round8(x);
+    const uint4 w = __builtin_bit_cast(uint4, hi);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[2 * e] -= bf16_lo_f32(u[e]); x[2 * e + 1] -= bf16_hi_f32(u[e]); }
+    return hi;
+}
+
+// 16 bytes of a row of `dim` elements from element d on, zero behind its end
+template <class T>
+__device__ __forceinline__ uint4 decay_load16(const T* row, int d, int dim, bool vec)
+{
+    constexpr int FE = DecayMma<T>::FE;
+    if (vec) return d < dim ? *(const uint4*)(row + d) : uint4{0, 0, 0, 0};
+    union { uint4 u; T e[FE]; } x;
+    x.u = uint4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < FE; ++i) if (d + i < dim) x.e[i] = row[d + i];
+    return x.u;
+}
+
+// the largest magnitude's bits, per element: an exponent of all ones is a value that is not finite
+template <class T>
+__device__ __forceinline__ uint32_t decay_magnitude(uint32_t seen, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) { const uint32_t m = w & 0x7fffffffu; return m > seen ? m : seen; }
+    else {
+        typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushortx2, seen), __builtin_bit_cast(ushortx2, w & 0x7fff7fffu)));
+    }
+}
+template <class T>
+__device__ __forceinline__ bool decay_not_finite(uint32_t seen)
+{
+    if constexpr (sizeof(T) == 4) return seen >= 0x7f800000u;
+    else return (seen & 0xffffu) >= 0x7f80u || (seen >> 16) >= 0x7f80u;
+}
+
+template <class T, int DK, int DVT, bool OUT> struct DecayLds {
+    static constexpr int C = DecayMma<T>::C, FE = DecayMma<T>::FE, PAD = FE;      // rows 16 bytes longer: operands of 16 rows fall on different banks
+    static constexpr int KROW = DK + PAD, CROW = C + PAD, PARTS = sizeof(T) == 4 ? 1 : 2;
+    static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (C * KROW > PARTS * C * CROW ? C * KROW : PARTS * C * CROW) : 0;
+    // queries; keys, later the scores' parts; keys and values with their steps side by side
+    static constexpr int Q = 0, K = NQ, KT = K + NK, VT = KT + DK * CROW, END = VT + DVT * CROW;
+    static constexpr size_t BYTES = (size_t)END * sizeof(T) + (2 * C + 8) * sizeof(float) + 16;
+};
+
+// OUT: outputs and the state; else what every segment adds to the state.
+template <class T, int DK, int DVT, bool OUT>
+__global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chunk_kernel(DecayArgs p)
+{
+    typedef DecayMma<T> M;
+    typedef typename M::Frag Frag;
+    typedef DecayLds<T, DK, DVT, OUT> L;
+    constexpr int C = M::C, FE = M::FE, KS = M::KS;
+    constexpr int MT = DK / 16, NT = DVT / 64, IT = C / 16, JS = C / KS;     // state tiles a column; columns tiles a wavefront; step tiles; depth of a chunk
+    constexpr int KB = (C / FE) * (DK / FE), VB = (C / FE) * (DVT / FE);     // FE x FE blocks of keys and values
+    constexpr int BL = (KB + VB + 255) / 256, QL = C * (DK / FE) / 256;      // blocks and query vectors a thread
+    extern __shared__ __attribute__((aligned(16))) char decay_lds[];
+    T* const lds = (T*)decay_lds;
+    T* const ldsq = lds + L::Q; T* const ldsk = lds + L::K; T* const ldskt = lds + L::KT; T* const ldsvt = lds + L::VT;
+    float* const pw = (float*)(lds + L::END);                // powers 0 .. C
+    float* const wend = pw + C + 4;                          // weight of step j in the state behind the chunk
+    uint64_t* const flags = (uint64_t*)(wend + C + 4);       // [0]: steps with a flag, [1]: a value is not finite
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, lg = lane >> 4;
+    const int tiles = (p.dv + DVT - 1) / DVT;
+    // neighbours (column tiles, heads of one key head) on one die: their keys and values meet in its cache
+    const uint32_t total = gridDim.x, xcd = blockIdx.x & 7, per = total >> 3, more = total & 7;
+    uint32_t id = xcd * per + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
+    const int tile = id % tiles; id /= tiles;
+    const int grp = p.H / p.KV;
+    const int hg = id % grp; id /= grp;
+    const int seg = id % p.segments; id /= p.segments;
+    const int hk = id % p.KV, b = id / p.KV, h = hk * grp + hg;
+    const int bh = b * p.H + h, col0 = tile * DVT;
+    const int len = decay_length(p, b);
+    const int begin = seg * p.segment_steps, end = min(len, begin + p.segment_steps);
+    const bool split = p.segments > 1;
+    if (OUT && split && begin >= end) return;                // (the scan has the state)
+
+    if (tid == 0) flags[1] = 0;
+    for (int n = tid; n <= C; n += 256) {
+        double g = (double)p.decay[h], r = 1.0;
+        for (int e = n; e; e >>= 1, g *= g) if (e & 1) r *= g;
+        pw[n] = (float)r;
+    }
+    const size_t state = (size_t)p.dk * p.dv;
+    floatx4 S[MT][NT];
+    {
+        const float* src = !OUT ? nullptr : split ? p.seg_state + ((size_t)bh * p.segments + seg) * state : p.s_in ? p.s_in + bh * state : nullptr;
+        if (OUT && !split && p.done && len > 0 && p.done[b]) src = nullptr;       // the first step starts anew: what is there is not read
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = decay_row<T>(m, 4 * lg + r), col = col0 + (wave * NT + n) * 16 + ln;
+                    S[m][n][r] = src && row < p.dk && col < p.dv ? src[(size_t)row * p.dv + col] : 0.0f;
+                }
+    }
+    const T* const q = (const T*)p.q + (int64_t)b * p.q_b + (int64_t)h * p.dk;
+    const T* const k = (const T*)p.k + (int64_t)b * p.k_b + (int64_t)hk * p.dk;
+    const T* const v = (const T*)p.v + (int64_t)b * p.v_b + (int64_t)hk * p.dv + col0;
+    T* const o = (T*)p.out + (int64_t)b * p.o_b + (int64_t)h * p.dv + col0;
+    const int dvt = min(DVT, p.dv - col0);
+
+    uint4 blk[BL][FE], qv[OUT ? QL : 1];
+    uint8_t flag = 0;
+    auto fetch = [&](int t0, int c) {                        // steps t0 .. t0 + c, zero behind them
+#pragma unroll
+        for (int i = 0; i < BL; ++i) {
+            const int idx = tid + 256 * i, is_v = idx >= KB, at = is_v ? idx - KB : idx;
+            const int jb = at % (C / FE) * FE, d = at / (C / FE) * FE;
+            if (idx >= KB + VB) continue;
+#pragma unroll
+            for (int j = 0; j < FE; ++j) {
+                blk[i][j] = uint4{0, 0, 0, 0};
+                if (jb + j < c) {
+                    const int64_t t = t0 + jb + j;
+                    blk[i][j] = is_v ? decay_load16<T>(v + t * p.v_t, d, dvt, p.vec_v) : decay_load16<T>(k + t * p.k_t, d, p.dk, p.vec_k);
+                }
+            }
+        }
+        if constexpr (OUT)
+#pragma unroll
+            for (int i = 0; i < QL; ++i) {
+                const int idx = tid + 256 * i, j = idx / (DK / FE), d = idx % (DK / FE) * FE;
+                qv[i] = j < c ? decay_load16<T>(q + (int64_t)(t0 + j) * p.q_t, d, p.dk, p.vec_q) : uint4{0, 0, 0, 0};
+            }
+        flag = 0;
+        if (p.done && tid < c) flag = p.done[(int64_t)(t0 + tid) * p.B + b];
+    };
+    auto stage = [&](int c) {
+        uint32_t seen = 0;
+#pragma unroll
+        for (int i = 0; i < BL; ++i) {
+            const int idx = tid + 256 * i, is_v = idx >= KB, at = is_v ? idx - KB : idx;
+            const int jb = at % (C / FE) * FE, d = at / (C / FE) * FE;
+            if (idx >= KB + VB) continue;
+#pragma unroll
+            for (int j = 0; j < FE; ++j) {
+                const uint4 w = blk[i][j];
+                seen = decay_magnitude<T>(decay_magnitude<T>(decay_magnitude<T>(decay_magnitude<T>(seen, w.x), w.y), w.z), w.w);
+                if (OUT && !is_v) *(uint4*)(ldsk + (jb + j) * L::KROW + d) = w;
+            }
+            T* const to = (is_v ? ldsvt : ldskt) + d * L::CROW + jb;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    auto pick = [&](const uint4& w) { return e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w; };
+                    *(uint4*)(to + e * L::CROW) = uint4{pick(blk[i][0]), pick(blk[i][1]), pick(blk[i][2]), pick(blk[i][3])};
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    auto word = [&](const uint4& w) { return e / 2 == 0 ? w.x : e / 2 == 1 ? w.y : e / 2 == 2 ? w.z : w.w; };
+                    uint32_t o4[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)              // the two steps' halves side by side
+                        o4[j] = __builtin_amdgcn_perm(word(blk[i][2 * j + 1]), word(blk[i][2 * j]), e & 1 ? 0x07060302u : 0x05040100u);
+                    *(uint4*)(to + e * L::CROW) = uint4{o4[0], o4[1], o4[2], o4[3]};
+                }
+            }
+        }
+        if constexpr (OUT)
+#pragma unroll
+            for (int i = 0; i < QL; ++i) {
+                const int idx = tid + 256 * i, j = idx / (DK / FE), d = idx % (DK / FE) * FE;
+                *(uint4*)(ldsq + j * L::KROW + d) = qv[i];
+            }
+        if (wave == 0) {                                     // (c <= 64: one wavefront holds every step's flag)
+            const uint64_t mask = __ballot(flag != 0);
+            if (lane == 0) flags[0] = mask;
+            if (lane < C) wend[lane] = lane < c && (mask >> lane >> 1) == 0 ? pw[c - 1 - lane] : 0.0f;
+        }
+        if (decay_not_finite<T>(seen)) flags[1] = 1;
+    };
+
+    float factor = 1.0f, cut = 0.0f;                         // of the segment so far
+    int single = 0;                                          // steps still to be done one by one
+    int t0 = begin, c = min(C, end - begin);
+    if (c > 0) fetch(t0, c);
+    __syncthreads();                                         // the table of powers
+    while (t0 < end) {
+        stage(c);
+        __syncthreads();
+        const uint64_t mask = flags[0];
+        if (flags[1]) {                                      // (uniform)
+            __syncthreads();
+            if (tid == 0) flags[1] = 0;
+            if (c > 1) {
+                single = c; c = 1;
+                fetch(t0, c);
+                __syncthreads();
+                continue;
+            }
+        }
+        if (single > 0) --single;
+        const int next = t0 + c, nc = min(single > 0 ? 1 : C, end - next);
+        if (nc > 0) fetch(next, nc);                         // on its way while this chunk is multiplied
+
+        // the values of the wavefront's columns
+        Frag vt[NT][JS];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int ks = 0; ks < JS; ++ks) vt[n][ks] = *(const Frag*)(ldsvt + ((wave * NT + n) * 16 + ln) * L::CROW + ks * KS + FE * lg);
+
+        if constexpr (OUT) {
+            // scores, transposed: lane: step i = 16 it + ln, four consecutive steps j
+            constexpr int SC = IT == 4 ? 4 : 1;              // tiles a wavefront: row `it` = wave of four, or one of two x two
+            floatx4 sc[SC];
+            const int it = IT == 4 ? wave : wave >> 1;
+#pragma unroll
+            for (int x = 0; x < SC; ++x) {
+                const int jt = IT == 4 ? x : wave & 1;
+                sc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+                if (jt > it) continue;                       // (uniform a wavefront)
+#pragma unroll
+                for (int d = 0; d < DK; d += KS) {
+                    const Frag fk = *(const Frag*)(ldsk + (16 * jt + ln) * L::KROW + d + FE * lg);
+                    const Frag fq = *(const Frag*)(ldsq + (16 * it + ln) * L::KROW + d + FE * lg);
+                    sc[x] = M::mma(fk, fq, sc[x]);
+                }
+            }
+            __syncthreads();                                 // keys are read: scores take their place
+            {
+                const int i = 16 * it + ln;
+                const uint64_t upto = mask & ((2ull << i) - 1);
+                const int low = upto ? 63 - __builtin_clzll(upto) : 0;            // steps j from the last flag on
+#pragma unroll
+                for (int x = 0; x < SC; ++x) {
+                    const int jt = IT == 4 ? x : wave & 1;
+                    floatx4 f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * jt + 4 * lg + r;
+                        f[r] = j <= i && j >= low ? sc[x][r] * pw[j <= i ? i - j : 0] : 0.0f;
+                    }
+                    T* const to = ldsk + i * L::CROW + 16 * jt + 4 * lg;
+                    if constexpr (sizeof(T) == 4) *(floatx4*)to = f;
+                    else {
+                        const bf16x4 hi = to_bf16x4(f);
+                        const floatx4 hf = to_floatx4(hi);
+                        *(bf16x4*)to = hi;
+                        *(bf16x4*)(to + C * L::CROW) = to_bf16x4(f - hf);
+                    }
+                }
+            }
+            // queries x state, transposed: lane: four consecutive columns, step i = 16 it + ln
+            floatx4 acc[IT][NT];
+#pragma unroll
+            for (int it2 = 0; it2 < IT; ++it2)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[it2][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < DK / KS; ++d) {
+                Frag s0[NT], s1[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if constexpr (sizeof(T) == 4) s0[n] = S[d][n];
+                    else {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = S[2 * d + (e >> 2)][n][e & 3];
+                        s0[n] = decay_split8(x);
+                        s1[n] = decay_round8(x);
+                    }
+                }
+#pragma unroll
+                for (int it2 = 0; it2 < IT; ++it2) {
+                    const Frag fq = *(const Frag*)(ldsq + (16 * it2 + ln) * L::KROW + d * KS + FE * lg);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        acc[it2][n] = M::mma(s0[n], fq, acc[it2][n]);
+                        if constexpr (sizeof(T) == 2) acc[it2][n] = M::mma(s1[n], fq, acc[it2][n]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int it2 = 0; it2 < IT; ++it2) {
+                const int i = 16 * it2 + ln;
+                const bool reached = (mask & ((2ull << i) - 1)) == 0;
+                const float w = pw[i + 1];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[it2][n][r] = reached ? acc[it2][n][r] * w : 0.0f;
+            }
+            __syncthreads();                                 // the scores are there
+#pragma unroll
+            for (int it2 = 0; it2 < IT; ++it2)
+#pragma unroll
+                for (int ks = 0; ks < JS; ++ks) {
+                    if (ks * KS > 16 * it2) continue;
+                    const T* const at = ldsk + (16 * it2 + ln) * L::CROW + ks * KS + FE * lg;
+                    const Frag p0 = *(const Frag*)at;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(vt[n][ks], p0, acc[it2][n]);
+                    if constexpr (sizeof(T) == 2) {
+                        const Frag p1 = *(const Frag*)(at + C * L::CROW);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(vt[n][ks], p1, acc[it2][n]);
+                    }
+                }
+#pragma unroll
+            for (int it2 = 0; it2 < IT; ++it2) {
+                const int i = 16 * it2 + ln;
+                if (i >= c) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int col = (wave * NT + n) * 16 + 4 * lg;
+                    const floatx4 f = acc[it2][n] * p.scale;
+                    T* const to = o + (int64_t)(t0 + i) * p.o_t + col;
+                    if (p.vec_o && col + 4 <= dvt) {
+                        if constexpr (sizeof(T) == 4) *(floatx4*)to = f;
+                        else *(bf16x4*)to = to_bf16x4(f);
+                    } else
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) if (col + r < dvt) to[r] = (T)f[r];
+                }
+            }
+        }
+
+        // the state behind the chunk
+        {
+            const bool any = mask != 0;
+            const float g = pw[c];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[m][n][r] = any ? 0.0f : S[m][n][r] * g;
+            factor = factor * g;
+            if (any) cut = 1.0f;
+        }
+#pragma unroll
+        for (int ks = 0; ks < JS; ++ks) {
+            Frag w0[NT], w1[NT], w2[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const floatx4 wa = *(const floatx4*)(wend + ks * KS + FE * lg);
+                if constexpr (sizeof(T) == 4) w0[n] = vt[n][ks] * wa;
+                else {
+                    const floatx4 wb = *(const floatx4*)(wend + ks * KS + FE * lg + 4);
+                    const uint4 u = __builtin_bit_cast(uint4, vt[n][ks]);
+                    float x[8] = {bf16_lo_f32(u.x) * wa[0], bf16_hi_f32(u.x) * wa[1], bf16_lo_f32(u.y) * wa[2], bf16_hi_f32(u.y) * wa[3],
+                                  bf16_lo_f32(u.z) * wb[0], bf16_hi_f32(u.z) * wb[1], bf16_lo_f32(u.w) * wb[2], bf16_hi_f32(u.w) * wb[3]};
+                    w0[n] = decay_split8(x);
+                    w1[n] = decay_split8(x);
+                    w2[n] = decay_round8(x);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const Frag fk = *(const Frag*)(ldskt + decay_row<T>(m, ln) * L::CROW + ks * KS + FE * lg);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    S[m][n] = M::mma(fk, w0[n], S[m][n]);
+                    if constexpr (sizeof(T) == 2) {
+                        S[m][n] = M::mma(fk, w1[n], S[m][n]);
+                        S[m][n] = M::mma(fk, w2[n], S[m][n]);
+                    }
+                }
+            }
+        }
+        __syncthreads();                                     // everything staged is read
+        t0 = next;
+        c = nc;
+    }
+
+    if (OUT && split) return;
+    float* const dst = OUT ? p.s_out + bh * state : p.seg_state + ((size_t)bh * p.segments + seg) * state;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = decay_row<T>(m, 4 * lg + r), col = col0 + (wave * NT + n) * 16 + ln;
+                if (row < p.dk && col < p.dv) dst[(size_t)row * p.dv + col] = S[m][n][r];
+            }
+    if (!OUT && tile == 0 && tid == 0) p.seg_factor[(size_t)bh * p.segments + seg] = make_float2(factor, cut);
+}
+
+// The states in front of the segments, in place of what the segments add, and the state behind the last.
+__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs p)
+{
+    const size_t state = (size_t)p.dk * p.dv;
+    const uint32_t blocks = (uint32_t)((state + 255) / 256);
+    const uint32_t bh = blockIdx.x / blocks;
+    const size_t at = (size_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+    if (at >= state) return;
+    float s = p.s_in ? p.s_in[bh * state + at] : 0.0f;
+    float* seg = p.seg_state + (size_t)bh * p.segments * state + at;
+    const float2* f = p.seg_factor + (size_t)bh * p.segments;
+    constexpr int U = 8;
+    for (int i = 0; i < p.segments; i += U) {
+        float add[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (i + u < p.segments) add[u] = seg[(i + u) * state];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u < p.segments) {
+                seg[(i + u) * state] = s;
+                const float2 g = f[i + u];
+                s = (g.y != 0.0f ? 0.0f : g.x * s) + add[u];
+            }
+    }
+    p.s_out[bh * state + at] = s;
+}
+
+// ---- choice and layout of a call ----
+
+struct DecayPlan {
+    bool chunks;                 // else step by step
+    int dk, dvt;                 // the kernel's sizes
+    int segments, segment_steps;
+    size_t factor_at, workspace; // bytes: where the factors stand, all
+};
+
+constexpr int DECAY_SHORT = 8;   // steps up to which the recurrence is walked
+
+static inline DecayPlan decay_plan(int dtype, int T, int B, int H, int dk, int dv)
+{
+    DecayPlan q{};
+    q.segments = 1; q.segment_steps = T;
+    q.chunks = T > DECAY_SHORT;
+    if (!q.chunks) return q;
+    q.dk = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
+    q.dvt = dv <= 64 || q.dk == 256 ? 64 : 128;
+    const int C = dtype == SEED_DTYPE_FP32 ? DecayMma<float>::C : DecayMma<__bf16>::C;
+    // Two workgroups a compute unit are wanted.  Fewer states than that: the time axis in segments, but of no less than
+    // four chunks (a segment's keys and values are read once more, its state travels four times).
+    const int64_t units = (int64_t)B * H * ((dv + q.dvt - 1) / q.dvt);
+    const int64_t want = (512 + units - 1) / units, most = T / (4 * C);
+    const int64_t n = want < most ? want : most;
+    if (n > 1) {
+        const int steps = (int)(((T + n - 1) / n + C - 1) / C * C);
+        q.segments = (T + steps - 1) / steps; q.segment_steps = steps;
+    }
+    if (q.segments > 1) {
+        q.factor_at = ((size_t)B * H * q.segments * dk * dv * sizeof(float) + 255) / 256 * 256;
+        q.workspace = q.factor_at + (size_t)B * H * q.segments * sizeof(float2);
+    }
+    return q;
+}
+
+template <class T, int DK, int DVT>
+static hipError_t decay_launch_chunks(const DecayArgs& p, hipStream_t s)
+{
+    const unsigned tiles = (p.dv + DVT - 1) / DVT, grid = (unsigned)((size_t)p.B * p.H * p.segments * tiles);
+    // (more than 64 KiB of LDS has to be asked for, once a kernel and device; asking again changes nothing)
+    auto go = [&](auto out) -> hipError_t {
+        constexpr bool OUT = decltype(out)::value;
+        constexpr size_t lds = DecayLds<T, DK, DVT, OUT>::BYTES;
+        if constexpr (lds > 65536) {
+            hipError_t e = hipFuncSetAttribute((const void*)decay_chunk_kernel<T, DK, DVT, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL((decay_chunk_kernel<T, DK, DVT, OUT>), dim3(grid), dim3(256), lds, s, p);
+        return hipSuccess;
+    };
+    if (p.segments > 1) {
+        hipError_t e = go(std::false_type{});
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(decay_scan_kernel, dim3((unsigned)((size_t)p.B * p.H * (((size_t)p.dk * p.dv + 255) / 256))), dim3(256), 0, s, p);
+    }
+    return go(std::true_type{});
+}
+
+template <class T>
+static hipError_t decay_launch(const DecayArgs& p, const DecayPlan& q, hipStream_t s)
+{
+    if (q.chunks) {
+        if (q.dk == 64) return q.dvt == 64 ? decay_launch_chunks<T, 64, 64>(p, s) : decay_launch_chunks<T, 64, 128>(p, s);
+        if (q.dk == 128) return q.dvt == 64 ? decay_launch_chunks<T, 128, 64>(p, s) : decay_launch_chunks<T, 128, 128>(p, s);
+        return decay_launch_chunks<T, 256, 64>(p, s);
+    }
     const unsigned grid = (unsigned)((size_t)p.B * p.H * ((p.dv + DECAY_COLS - 1) / DECAY_COLS));
     if (p.dk <= 64) hipLaunchKernelGGL((decay_recurrent_kernel<T, 64>), dim3(grid), dim3(256), 0, s, p);
     else if (p.dk <= 128) hipLaunchKernelGGL((decay_recurrent_kernel<T, 128>), dim3(grid), dim3(256), 0, s, p);
     else hipLaunchKernelGGL((decay_recurrent_kernel<T, 256>), dim3(grid), dim3(256), 0, s, p);
+    return hipSuccess;
 }
 
 }  // namespace seedinf

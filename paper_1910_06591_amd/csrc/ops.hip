@@ -95,8 +95,8 @@ static bool strided_overlap(const StridedArray& a, const StridedArray& b, int64_
 
 extern "C" size_t seed_op_decay_workspace(const seed_decay_t* desc)
 {
-    if (decay_check(desc) != SEED_OK) return 0;
-    return 0;
+    if (decay_check(desc) != SEED_OK || desc->rows == 0) return 0;
+    return decay_plan(desc->dtype, desc->steps, desc->rows, desc->heads, desc->key_dim, desc->value_dim).workspace;
 }
 
 extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, const void* k, const void* v, const float* decay,
@@ -134,8 +134,21 @@ extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, con
     p.q_t = d->q_step; p.q_b = d->q_row; p.k_t = d->k_step; p.k_b = d->k_row; p.v_t = d->v_step; p.v_b = d->v_row; p.o_t = d->out_step; p.o_b = d->out_row;
     p.T = d->steps; p.B = d->rows; p.H = d->heads; p.KV = d->kv_heads; p.dk = d->key_dim; p.dv = d->value_dim; p.scale = d->scale;
     p.vec_state = d->value_dim % 4 == 0 && op_aligned(state_in, 16) && op_aligned(state_out, 16);
-    if (d->dtype == SEED_DTYPE_FP32) decay_launch<float>(p, (hipStream_t)hip_stream);
-    else decay_launch<__bf16>(p, (hipStream_t)hip_stream);
+    const DecayPlan plan = decay_plan(d->dtype, d->steps, d->rows, d->heads, d->key_dim, d->value_dim);
+    p.segments = plan.segments; p.segment_steps = plan.segment_steps;
+    if (plan.workspace) {
+        p.seg_state = (float*)workspace;
+        p.seg_factor = (float2*)((char*)workspace + plan.factor_at);
+    }
+    // n elements from every head on, at a time
+    auto whole = [&](const void* a, int64_t step, int64_t row, int dim, int n) {
+        return op_aligned(a, n * size) && dim % n == 0 && (d->steps == 1 || step % n == 0) && (d->rows == 1 || row % n == 0);
+    };
+    const int n16 = (int)(16 / size);
+    p.vec_q = whole(q, p.q_t, p.q_b, p.dk, n16); p.vec_k = whole(k, p.k_t, p.k_b, p.dk, n16); p.vec_v = whole(v, p.v_t, p.v_b, p.dv, n16);
+    p.vec_o = whole(out, p.o_t, p.o_b, p.dv, 4);
+    const hipError_t e = d->dtype == SEED_DTYPE_FP32 ? decay_launch<float>(p, plan, (hipStream_t)hip_stream) : decay_launch<__bf16>(p, plan, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return op_fail(SEED_ERR_DEVICE, "launch failed: %s", hipGetErrorString(e));
     return op_launched();
 }
 
