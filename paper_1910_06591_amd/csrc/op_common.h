@@ -10,9 +10,9 @@
 
 namespace seedinf {
 
-template <class T> struct ElemVec;
-template <> struct ElemVec<float> { static constexpr int N = 4; typedef floatx4 V; };
-template <> struct ElemVec<__bf16> { static constexpr int N = 8; typedef bf16x8 V; };
+// 16 bytes as they travel.  (HIP's uint4 is a class: choosing between two of them chooses between their addresses, which
+// takes them out of registers.)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // x / (1 + exp(-x)); the reciprocal instruction is good to one unit in the last place
 __device__ __forceinline__ float op_silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }

@@ -1,6 +1,7 @@
 // Linear attention with a decay for each head: a recurrent core whose state is a matrix per head,
 //   S_t = g S_{t-1} + k_t v_t^T   (S_{t-1} taken as zero where done_t is set),    o_t = scale q_t^T S_t.
 #pragma once
+#include <atomic>
 #include <type_traits>
 
 #include "op_common.h"
@@ -19,8 +20,8 @@ struct DecayArgs {
     int T, B, H, KV, dk, dv;
     float scale;
     int vec_state;               // dv and the states' addresses allow 16-byte accesses
-    int vec_q, vec_k, vec_v;     // every step's heads are 16-byte aligned, dims whole vectors
-    int vec_o;                   // four outputs can be stored at once
+    int vec_in;                  // q, k and v: every head is 16-byte aligned and whole 16 bytes, a step's stride is below 2^25 bytes
+    int vec_o;                   // 16 bytes of outputs can be stored at once
     int segments, segment_steps; // the time axis in parts that are worked on side by side; 1: not split
     float* seg_state;            // [rows, heads, segments, dk, dv]: what a segment adds to the state, then the state in front of it
     float2* seg_factor;          // [rows, heads, segments]: (power of the decay over the segment, 1 if a flag lies in it)
@@ -164,21 +165,20 @@ __device__ __forceinline__ bf16x8 decay_round8(const float (&x)[8]) { return to_
 __device__ __forceinline__ bf16x8 decay_split8(float (&x)[8])
 {
     const bf16x8 hi = decay_round8(x);
-    const uint4 w = __builtin_bit_cast(uint4, hi);
+    const u32x4 w = __builtin_bit_cast(u32x4, hi);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) { x[2 * e] -= bf16_lo_f32(u[e]); x[2 * e + 1] -= bf16_hi_f32(u[e]); }
     return hi;
 }
 
-// 16 bytes of a row of `dim` elements from element d on, zero behind its end
+// FE elements of a row of `dim` elements from element d on, one by one, zero behind its end
 template <class T>
-__device__ __forceinline__ uint4 decay_load16(const T* row, int d, int dim, bool vec)
+__device__ __forceinline__ u32x4 decay_load16(const T* row, int d, int dim)
 {
     constexpr int FE = DecayMma<T>::FE;
-    if (vec) return d < dim ? *(const uint4*)(row + d) : uint4{0, 0, 0, 0};
-    union { uint4 u; T e[FE]; } x;
-    x.u = uint4{0, 0, 0, 0};
+    union { u32x4 u; T e[FE]; } x;
+    x.u = u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < FE; ++i) if (d + i < dim) x.e[i] = row[d + i];
     return x.u;
@@ -201,34 +201,57 @@ __device__ __forceinline__ bool decay_not_finite(uint32_t seen)
     else return (seen & 0xffffu) >= 0x7f80u || (seen >> 16) >= 0x7f80u;
 }
 
+// LDS rows of R bytes without padding; 16-byte pieces of a 256-byte line change places with the row, so that the 16
+// rows (lanes) and 4 pieces (lane groups) of an operand read fall on different banks.
+template <int R> __device__ __forceinline__ uint32_t decay_at(int row, int piece)
+{
+    if constexpr (R == 128) return (uint32_t)((row >> 1) * 256 + ((((row & 1) << 3) | piece) ^ ((row >> 1) & 7)) * 16);
+    else return (uint32_t)(row * R + ((piece & ~15) | ((piece ^ row) & 15)) * 16);
+}
+// The operand of rows 16 t + ln and pieces 4 ks + lg: `x` is decay_operand_x<R>(ln, lg); t and ks are constants.
+template <int R> __device__ __forceinline__ uint32_t decay_operand_x(int ln, int lg) { return decay_at<R>(ln, lg); }
+template <int R> __device__ __forceinline__ uint32_t decay_operand(uint32_t x, int t, int ks)
+{
+    if constexpr (R == 128) return (x ^ (uint32_t)(ks * 64)) + (uint32_t)(t * 16 * R);
+    else return (x ^ (uint32_t)((ks & 3) * 64)) + (uint32_t)(t * 16 * R + (ks >> 2) * 256);
+}
+
 template <class T, int DK, int DVT, bool OUT> struct DecayLds {
-    static constexpr int C = DecayMma<T>::C, FE = DecayMma<T>::FE, PAD = FE;      // rows 16 bytes longer: operands of 16 rows fall on different banks
-    static constexpr int KROW = DK + PAD, CROW = C + PAD, PARTS = sizeof(T) == 4 ? 1 : 2;
-    static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (C * KROW > PARTS * C * CROW ? C * KROW : PARTS * C * CROW) : 0;
-    // queries; keys, later the scores' parts; keys and values with their steps side by side
+    static constexpr int C = DecayMma<T>::C;
+    static constexpr int KROW = DK * (int)sizeof(T), CROW = C * (int)sizeof(T), PARTS = sizeof(T) == 4 ? 1 : 2;      // bytes a row
+    static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (KROW > PARTS * CROW ? C * KROW : PARTS * C * CROW) : 0;
+    // queries; keys, later the scores' parts; keys and values with their steps side by side; tables
     static constexpr int Q = 0, K = NQ, KT = K + NK, VT = KT + DK * CROW, END = VT + DVT * CROW;
-    static constexpr size_t BYTES = (size_t)END * sizeof(T) + (2 * C + 8) * sizeof(float) + 16;
+    static constexpr size_t BYTES = (size_t)END + (2 * C + 8) * sizeof(float) + 16;
+    static constexpr int RESIDENT = BYTES <= 80 * 1024 ? 2 : 1;          // workgroups a compute unit
 };
 
-// OUT: outputs and the state; else what every segment adds to the state.
-template <class T, int DK, int DVT, bool OUT>
-__global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chunk_kernel(DecayArgs p)
+// the row of the transposed arrays that element d stands in: the order of the accumulators' rows (decay_row's inverse)
+template <class T> __device__ __forceinline__ int decay_place(int d)
+{
+    if constexpr (sizeof(T) == 4) return d;
+    else return (d & ~31) | ((d & 4) << 2) | ((d & 24) >> 1) | (d & 3);
+}
+
+// OUT: outputs and the state; else what every segment adds to the state.  VEC: 16-byte loads, a step's stride of less
+// than 2^25 bytes (a chunk's offsets are 32 bits from a base that all threads share).
+template <class T, int DK, int DVT, bool OUT, bool VEC>
+__global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void decay_chunk_kernel(DecayArgs p)
 {
     typedef DecayMma<T> M;
     typedef typename M::Frag Frag;
     typedef DecayLds<T, DK, DVT, OUT> L;
-    constexpr int C = M::C, FE = M::FE, KS = M::KS;
+    constexpr int C = M::C, FE = M::FE, KS = M::KS, KROW = L::KROW, CROW = L::CROW;
     constexpr int MT = DK / 16, NT = DVT / 64, IT = C / 16, JS = C / KS;     // state tiles a column; columns tiles a wavefront; step tiles; depth of a chunk
     constexpr int KB = (C / FE) * (DK / FE), VB = (C / FE) * (DVT / FE);     // FE x FE blocks of keys and values
     constexpr int BL = (KB + VB + 255) / 256, QL = C * (DK / FE) / 256;      // blocks and query vectors a thread
-    extern __shared__ __attribute__((aligned(16))) char decay_lds[];
-    T* const lds = (T*)decay_lds;
-    T* const ldsq = lds + L::Q; T* const ldsk = lds + L::K; T* const ldskt = lds + L::KT; T* const ldsvt = lds + L::VT;
-    float* const pw = (float*)(lds + L::END);                // powers 0 .. C
+    extern __shared__ __attribute__((aligned(256))) char decay_lds[];
+    char* const ldsq = decay_lds + L::Q; char* const ldsk = decay_lds + L::K; char* const ldskt = decay_lds + L::KT; char* const ldsvt = decay_lds + L::VT;
+    float* const pw = (float*)(decay_lds + L::END);          // powers 0 .. C
     float* const wend = pw + C + 4;                          // weight of step j in the state behind the chunk
     uint64_t* const flags = (uint64_t*)(wend + C + 4);       // [0]: steps with a flag, [1]: a value is not finite
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 15, lg = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 15, lg = lane >> 4;
     const int tiles = (p.dv + DVT - 1) / DVT;
     // neighbours (column tiles, heads of one key head) on one die: their keys and values meet in its cache
     const uint32_t total = gridDim.x, xcd = blockIdx.x & 7, per = total >> 3, more = total & 7;
@@ -261,7 +284,7 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = decay_row<T>(m, 4 * lg + r), col = col0 + (wave * NT + n) * 16 + ln;
+                    const int row = decay_row<T>(m, 4 * lg + r), col = col0 + decay_row<T>(wave * NT + n, ln);
                     S[m][n][r] = src && row < p.dk && col < p.dv ? src[(size_t)row * p.dv + col] : 0.0f;
                 }
     }
@@ -271,69 +294,120 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
     T* const o = (T*)p.out + (int64_t)b * p.o_b + (int64_t)h * p.dv + col0;
     const int dvt = min(DVT, p.dv - col0);
 
-    uint4 blk[BL][FE], qv[OUT ? QL : 1];
+    // Block `at` of keys or values: FE steps from j on, FE elements from d on.  The order spreads a wavefront's writes of
+    // both layouts over the banks and keeps 128 bytes of a row together in its reads.
+    auto block_j = [](int at) { return ((at & 1) | ((at >> 4 & 3) << 1)) * FE; };
+    auto block_d = [](int at) { return ((at >> 1 & 7) | (at >> 6 << 3)) * FE; };
+    u32x4 blk[BL][FE], qv[OUT && !VEC ? QL : 1];
     uint8_t flag = 0;
-    auto fetch = [&](int t0, int c) {                        // steps t0 .. t0 + c, zero behind them
+    // A thread's number that the compiler takes for a new one: addresses made from it are made where they are used (a few
+    // instructions each); held across the loop, all of them together take more registers than there are.
+    auto fresh = [](int x) { asm volatile("" : "+v"(x)); return x; };
+    auto fetch = [&](int t0, int c) __attribute__((always_inline)) {                        // steps t0 .. t0 + c; behind them and behind the dimensions: any value of the array
+        const int me = fresh(lane);
 #pragma unroll
         for (int i = 0; i < BL; ++i) {
-            const int idx = tid + 256 * i, is_v = idx >= KB, at = is_v ? idx - KB : idx;
-            const int jb = at % (C / FE) * FE, d = at / (C / FE) * FE;
-            if (idx >= KB + VB) continue;
+            const int first = wave * 64 + 256 * i, idx = first + me;
+            const bool is_v = first >= KB;                   // (KB is whole wavefronts)
+            const int at = is_v ? idx - KB : idx, j0 = block_j(at), d = block_d(at), dim = is_v ? dvt : p.dk;
+            if (first >= KB + VB) continue;
+            const int64_t step = is_v ? p.v_t : p.k_t;
+            const T* const base = (is_v ? v : k) + (int64_t)t0 * step;
+            if constexpr (VEC) {
+                const uint32_t dd = min(d, dim - FE);
+                if (c == C) {
+                    const uint32_t off = (uint32_t)(j0 * step + dd) * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int j = 0; j < FE; ++j) {
-                blk[i][j] = uint4{0, 0, 0, 0};
-                if (jb + j < c) {
-                    const int64_t t = t0 + jb + j;
-                    blk[i][j] = is_v ? decay_load16<T>(v + t * p.v_t, d, dvt, p.vec_v) : decay_load16<T>(k + t * p.k_t, d, p.dk, p.vec_k);
-                }
-            }
+                    for (int j = 0; j < FE; ++j) blk[i][j] = *(const u32x4*)((const char*)(base + j * step) + off);
+                } else
+#pragma unroll
+                    for (int j = 0; j < FE; ++j) blk[i][j] = *(const u32x4*)((const char*)base + (uint32_t)(min(j0 + j, c - 1) * step + dd) * (uint32_t)sizeof(T));
+            } else
+#pragma unroll
+                for (int j = 0; j < FE; ++j) blk[i][j] = decay_load16<T>(base + min(j0 + j, c - 1) * step, d, dim);
         }
-        if constexpr (OUT)
+        if constexpr (OUT && !VEC)
 #pragma unroll
             for (int i = 0; i < QL; ++i) {
-                const int idx = tid + 256 * i, j = idx / (DK / FE), d = idx % (DK / FE) * FE;
-                qv[i] = j < c ? decay_load16<T>(q + (int64_t)(t0 + j) * p.q_t, d, p.dk, p.vec_q) : uint4{0, 0, 0, 0};
+                const int idx = tid + 256 * i, j = min(idx / (DK / FE), c - 1), d = idx % (DK / FE) * FE;
+                qv[i] = decay_load16<T>(q + (t0 + j) * p.q_t, d, p.dk);
             }
         flag = 0;
         if (p.done && tid < c) flag = p.done[(int64_t)(t0 + tid) * p.B + b];
     };
-    auto stage = [&](int c) {
+    // The queries go straight to LDS, 64 pieces of 16 bytes at a time: lane l's lands at place l, so it fetches the piece
+    // that belongs there.  What stands behind the steps and behind key_dim is a repetition: outputs of steps that are not
+    // there are not stored, and the keys are zero there.
+    const uint32_t ldsq_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ldsq;
+    auto fetch_q = [&](int t0, int c) __attribute__((always_inline)) {
+        if constexpr (OUT && VEC) {
+            const T* const base = q + (int64_t)t0 * p.q_t;
+            const int me = fresh(lane);
+#pragma unroll
+            for (int i = 0; i < C * KROW / 4096; ++i) {
+                const int at = (wave * (C * KROW / 4096) + i) * 1024, byte = at + me * 16;
+                int j, piece;
+                if constexpr (KROW == 128) {
+                    const int line = byte >> 8, y = (me & 15) ^ (line & 7);
+                    j = 2 * line + (y >> 3); piece = y & 7;
+                } else {
+                    j = byte / KROW;
+                    const int slot = byte / 16 % (KROW / 16);
+                    piece = (slot & ~15) | ((slot ^ j) & 15);
+                }
+                g2lds16((const char*)base + (uint32_t)(min(j, c - 1) * p.q_t + min(piece * FE, p.dk - FE)) * (uint32_t)sizeof(T), ldsq_at + at);
+            }
+        }
+    };
+    auto stage = [&](int c) __attribute__((always_inline)) {
         uint32_t seen = 0;
+        const u32x4 zero = {0, 0, 0, 0};
+        const int me = fresh(lane);
 #pragma unroll
         for (int i = 0; i < BL; ++i) {
-            const int idx = tid + 256 * i, is_v = idx >= KB, at = is_v ? idx - KB : idx;
-            const int jb = at % (C / FE) * FE, d = at / (C / FE) * FE;
-            if (idx >= KB + VB) continue;
+            const int first = wave * 64 + 256 * i, idx = first + me;
+            const bool is_v = first >= KB;
+            const int at = is_v ? idx - KB : idx, j0 = block_j(at), d = block_d(at);
+            if (first >= KB + VB) continue;
+            if (c < C)
+#pragma unroll
+                for (int j = 0; j < FE; ++j) if (j0 + j >= c) blk[i][j] = zero;
+            if (VEC && (is_v ? dvt < DVT : p.dk < DK)) {
+                if (d >= (is_v ? dvt : p.dk))
+#pragma unroll
+                    for (int j = 0; j < FE; ++j) blk[i][j] = zero;
+            }
 #pragma unroll
             for (int j = 0; j < FE; ++j) {
-                const uint4 w = blk[i][j];
+                const u32x4 w = blk[i][j];
                 seen = decay_magnitude<T>(decay_magnitude<T>(decay_magnitude<T>(decay_magnitude<T>(seen, w.x), w.y), w.z), w.w);
-                if (OUT && !is_v) *(uint4*)(ldsk + (jb + j) * L::KROW + d) = w;
+                if (OUT && !is_v) *(u32x4*)(ldsk + decay_at<KROW>(j0 + j, d / FE)) = w;
             }
-            T* const to = (is_v ? ldsvt : ldskt) + d * L::CROW + jb;
+            char* const to = is_v ? ldsvt : ldskt;
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    auto pick = [&](const uint4& w) { return e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w; };
-                    *(uint4*)(to + e * L::CROW) = uint4{pick(blk[i][0]), pick(blk[i][1]), pick(blk[i][2]), pick(blk[i][3])};
+                    auto pick = [&](const u32x4& w) { return e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w; };
+                    *(u32x4*)(to + decay_at<CROW>(d + e, j0 / FE)) = u32x4{pick(blk[i][0]), pick(blk[i][1]), pick(blk[i][2]), pick(blk[i][3])};
                 }
             } else {
+                const int row = decay_place<T>(d);           // elements e: rows + (e & 3) + 16 (e >> 2)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    auto word = [&](const uint4& w) { return e / 2 == 0 ? w.x : e / 2 == 1 ? w.y : e / 2 == 2 ? w.z : w.w; };
+                    auto word = [&](const u32x4& w) { return e / 2 == 0 ? w.x : e / 2 == 1 ? w.y : e / 2 == 2 ? w.z : w.w; };
                     uint32_t o4[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j)              // the two steps' halves side by side
                         o4[j] = __builtin_amdgcn_perm(word(blk[i][2 * j + 1]), word(blk[i][2 * j]), e & 1 ? 0x07060302u : 0x05040100u);
-                    *(uint4*)(to + e * L::CROW) = uint4{o4[0], o4[1], o4[2], o4[3]};
+                    *(u32x4*)(to + decay_at<CROW>(row + (e & 3) + 16 * (e >> 2), j0 / FE)) = u32x4{o4[0], o4[1], o4[2], o4[3]};
                 }
             }
         }
-        if constexpr (OUT)
+        if constexpr (OUT && !VEC)
 #pragma unroll
             for (int i = 0; i < QL; ++i) {
-                const int idx = tid + 256 * i, j = idx / (DK / FE), d = idx % (DK / FE) * FE;
-                *(uint4*)(ldsq + j * L::KROW + d) = qv[i];
+                const int idx = tid + 256 * i, j = idx / (DK / FE), d = idx % (DK / FE);
+                *(u32x4*)(ldsq + decay_at<KROW>(j, d)) = qv[i];
             }
         if (wave == 0) {                                     // (c <= 64: one wavefront holds every step's flag)
             const uint64_t mask = __ballot(flag != 0);
@@ -342,21 +416,27 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
         }
         if (decay_not_finite<T>(seen)) flags[1] = 1;
     };
+    auto uniform64 = [](uint64_t x) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+    };
+    const uint32_t xk = decay_operand_x<KROW>(ln, lg), xc = decay_operand_x<CROW>(ln, lg);
 
     float factor = 1.0f, cut = 0.0f;                         // of the segment so far
     int single = 0;                                          // steps still to be done one by one
     int t0 = begin, c = min(C, end - begin);
-    if (c > 0) fetch(t0, c);
+    if (c > 0) { fetch_q(t0, c); fetch(t0, c); }
     __syncthreads();                                         // the table of powers
     while (t0 < end) {
         stage(c);
+        if constexpr (OUT && VEC) stage_wait();              // (the queries')
         __syncthreads();
-        const uint64_t mask = flags[0];
-        if (flags[1]) {                                      // (uniform)
+        const uint64_t mask = uniform64(flags[0]);
+        if (uniform64(flags[1])) {
             __syncthreads();
             if (tid == 0) flags[1] = 0;
             if (c > 1) {
                 single = c; c = 1;
+                fetch_q(t0, c);
                 fetch(t0, c);
                 __syncthreads();
                 continue;
@@ -364,33 +444,26 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
         }
         if (single > 0) --single;
         const int next = t0 + c, nc = min(single > 0 ? 1 : C, end - next);
-        if (nc > 0) fetch(next, nc);                         // on its way while this chunk is multiplied
 
-        // the values of the wavefront's columns
-        Frag vt[NT][JS];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int ks = 0; ks < JS; ++ks) vt[n][ks] = *(const Frag*)(ldsvt + ((wave * NT + n) * 16 + ln) * L::CROW + ks * KS + FE * lg);
-
+        floatx4 acc[IT][NT];
         if constexpr (OUT) {
             // scores, transposed: lane: step i = 16 it + ln, four consecutive steps j
             constexpr int SC = IT == 4 ? 4 : 1;              // tiles a wavefront: row `it` = wave of four, or one of two x two
             floatx4 sc[SC];
             const int it = IT == 4 ? wave : wave >> 1;
 #pragma unroll
-            for (int x = 0; x < SC; ++x) {
-                const int jt = IT == 4 ? x : wave & 1;
-                sc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-                if (jt > it) continue;                       // (uniform a wavefront)
+            for (int x = 0; x < SC; ++x) sc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int d = 0; d < DK; d += KS) {
-                    const Frag fk = *(const Frag*)(ldsk + (16 * jt + ln) * L::KROW + d + FE * lg);
-                    const Frag fq = *(const Frag*)(ldsq + (16 * it + ln) * L::KROW + d + FE * lg);
-                    sc[x] = M::mma(fk, fq, sc[x]);
+            for (int d = 0; d < DK / KS; ++d) {
+                const Frag fq = *(const Frag*)(ldsq + decay_operand<KROW>(xk, 0, d) + it * 16 * KROW);
+#pragma unroll
+                for (int x = 0; x < SC; ++x) {
+                    const int jt = IT == 4 ? x : wave & 1;
+                    if (jt <= it) sc[x] = M::mma(*(const Frag*)(ldsk + decay_operand<KROW>(xk, 0, d) + jt * 16 * KROW), fq, sc[x]);
                 }
             }
             __syncthreads();                                 // keys are read: scores take their place
+            if (nc > 0) fetch(next, nc);                     // on its way while the rest is multiplied
             {
                 const int i = 16 * it + ln;
                 const uint64_t upto = mask & ((2ull << i) - 1);
@@ -404,25 +477,26 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
                         const int j = 16 * jt + 4 * lg + r;
                         f[r] = j <= i && j >= low ? sc[x][r] * pw[j <= i ? i - j : 0] : 0.0f;
                     }
-                    T* const to = ldsk + i * L::CROW + 16 * jt + 4 * lg;
-                    if constexpr (sizeof(T) == 4) *(floatx4*)to = f;
+                    if constexpr (sizeof(T) == 4) *(floatx4*)(ldsk + decay_at<CROW>(i, 4 * jt + lg)) = f;
                     else {
+                        char* const to = ldsk + decay_at<CROW>(i, 2 * jt + (lg >> 1)) + 8 * (lg & 1);
                         const bf16x4 hi = to_bf16x4(f);
                         const floatx4 hf = to_floatx4(hi);
                         *(bf16x4*)to = hi;
-                        *(bf16x4*)(to + C * L::CROW) = to_bf16x4(f - hf);
+                        *(bf16x4*)(to + C * CROW) = to_bf16x4(f - hf);
                     }
                 }
             }
             // queries x state, transposed: lane: four consecutive columns, step i = 16 it + ln
-            floatx4 acc[IT][NT];
 #pragma unroll
             for (int it2 = 0; it2 < IT; ++it2)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[it2][n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int d = 0; d < DK / KS; ++d) {
-                Frag s0[NT], s1[NT];
+                Frag fq[IT], s0[NT], s1[NT];
+#pragma unroll
+                for (int it2 = 0; it2 < IT; ++it2) fq[it2] = *(const Frag*)(ldsq + decay_operand<KROW>(xk, it2, d));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     if constexpr (sizeof(T) == 4) s0[n] = S[d][n];
@@ -435,101 +509,123 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
                     }
                 }
 #pragma unroll
-                for (int it2 = 0; it2 < IT; ++it2) {
-                    const Frag fq = *(const Frag*)(ldsq + (16 * it2 + ln) * L::KROW + d * KS + FE * lg);
+                for (int it2 = 0; it2 < IT; ++it2)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        acc[it2][n] = M::mma(s0[n], fq, acc[it2][n]);
-                        if constexpr (sizeof(T) == 2) acc[it2][n] = M::mma(s1[n], fq, acc[it2][n]);
-                    }
-                }
+                    for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(s0[n], fq[it2], acc[it2][n]);
+                if constexpr (sizeof(T) == 2)
+#pragma unroll
+                    for (int it2 = 0; it2 < IT; ++it2)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(s1[n], fq[it2], acc[it2][n]);
+                __builtin_amdgcn_sched_barrier(0);           // (the state's parts are made where they are used)
             }
 #pragma unroll
             for (int it2 = 0; it2 < IT; ++it2) {
                 const int i = 16 * it2 + ln;
-                const bool reached = (mask & ((2ull << i) - 1)) == 0;
                 const float w = pw[i + 1];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[it2][n][r] = reached ? acc[it2][n][r] * w : 0.0f;
+                for (int n = 0; n < NT; ++n) acc[it2][n] *= w;
             }
-            __syncthreads();                                 // the scores are there
+            if (mask)                                        // (a uniform branch: most chunks have no flag)
 #pragma unroll
-            for (int it2 = 0; it2 < IT; ++it2)
+                for (int it2 = 0; it2 < IT; ++it2)
+                    if (mask & ((2ull << (16 * it2 + ln)) - 1))
 #pragma unroll
-                for (int ks = 0; ks < JS; ++ks) {
-                    if (ks * KS > 16 * it2) continue;
-                    const T* const at = ldsk + (16 * it2 + ln) * L::CROW + ks * KS + FE * lg;
-                    const Frag p0 = *(const Frag*)at;
+                        for (int n = 0; n < NT; ++n) acc[it2][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+            __syncthreads();                                 // the scores are there, and the queries are read
+            if (nc > 0) fetch_q(next, nc);
+        } else if (nc > 0) fetch(next, nc);
+
+        // the values of the wavefront's columns
+        Frag vt[NT][JS];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(vt[n][ks], p0, acc[it2][n]);
-                    if constexpr (sizeof(T) == 2) {
-                        const Frag p1 = *(const Frag*)(at + C * L::CROW);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(vt[n][ks], p1, acc[it2][n]);
+            for (int ks = 0; ks < JS; ++ks) vt[n][ks] = *(const Frag*)(ldsvt + decay_operand<CROW>(xc, n, ks) + wave * NT * 16 * CROW);
+
+        if constexpr (OUT) {
+            constexpr int PARTS = sizeof(T) == 4 ? 1 : 2;
+#pragma unroll
+            for (int ks = 0; ks < JS; ++ks)
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                    for (int it2 = 0; it2 < IT; ++it2) {
+                        if (ks * KS > 16 * it2) continue;
+                        const Frag f = *(const Frag*)(ldsk + decay_operand<CROW>(xc, it2, ks) + part * C * CROW);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(vt[n][ks], f, acc[it2][n]);
                     }
-                }
 #pragma unroll
             for (int it2 = 0; it2 < IT; ++it2) {
                 const int i = 16 * it2 + ln;
                 if (i >= c) continue;
+                T* const row = o + (int64_t)(t0 + i) * p.o_t;
+                if constexpr (sizeof(T) == 2 && NT == 2) {   // two tiles are eight consecutive columns
+                    const int col = 32 * wave + 8 * lg;
+                    if (p.vec_o && col + 8 <= dvt) {
+                        *(bf16x8*)(row + col) = to_bf16x8(acc[it2][0] * p.scale, acc[it2][1] * p.scale);
+                        continue;
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const int col = (wave * NT + n) * 16 + 4 * lg;
+                    const int col = decay_row<T>(wave * NT + n, 4 * lg);
                     const floatx4 f = acc[it2][n] * p.scale;
-                    T* const to = o + (int64_t)(t0 + i) * p.o_t + col;
                     if (p.vec_o && col + 4 <= dvt) {
-                        if constexpr (sizeof(T) == 4) *(floatx4*)to = f;
-                        else *(bf16x4*)to = to_bf16x4(f);
+                        if constexpr (sizeof(T) == 4) *(floatx4*)(row + col) = f;
+                        else *(bf16x4*)(row + col) = to_bf16x4(f);
                     } else
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) if (col + r < dvt) to[r] = (T)f[r];
+                        for (int r = 0; r < 4; ++r) if (col + r < dvt) row[col + r] = (T)f[r];
                 }
             }
         }
 
         // the state behind the chunk
-        {
-            const bool any = mask != 0;
-            const float g = pw[c];
+        if (mask) {
+            cut = 1.0f;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) S[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+        } else {
+            const float g = pw[c];
+            factor *= g;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[m][n][r] = any ? 0.0f : S[m][n][r] * g;
-            factor = factor * g;
-            if (any) cut = 1.0f;
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) S[m][n] *= g;
         }
 #pragma unroll
         for (int ks = 0; ks < JS; ++ks) {
-            Frag w0[NT], w1[NT], w2[NT];
+            constexpr int W = sizeof(T) == 4 ? 1 : 3;
+            Frag w[W][NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 wa = *(const floatx4*)(wend + ks * KS + FE * lg);
-                if constexpr (sizeof(T) == 4) w0[n] = vt[n][ks] * wa;
+                if constexpr (sizeof(T) == 4) w[0][n] = vt[n][ks] * wa;
                 else {
                     const floatx4 wb = *(const floatx4*)(wend + ks * KS + FE * lg + 4);
-                    const uint4 u = __builtin_bit_cast(uint4, vt[n][ks]);
+                    const u32x4 u = __builtin_bit_cast(u32x4, vt[n][ks]);
                     float x[8] = {bf16_lo_f32(u.x) * wa[0], bf16_hi_f32(u.x) * wa[1], bf16_lo_f32(u.y) * wa[2], bf16_hi_f32(u.y) * wa[3],
                                   bf16_lo_f32(u.z) * wb[0], bf16_hi_f32(u.z) * wb[1], bf16_lo_f32(u.w) * wb[2], bf16_hi_f32(u.w) * wb[3]};
-                    w0[n] = decay_split8(x);
-                    w1[n] = decay_split8(x);
-                    w2[n] = decay_round8(x);
+                    w[0][n] = decay_split8(x);
+                    w[1][n] = decay_split8(x);
+                    w[2][n] = decay_round8(x);
                 }
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const Frag fk = *(const Frag*)(ldskt + decay_row<T>(m, ln) * L::CROW + ks * KS + FE * lg);
+            for (int m = 0; m < MT; m += 4) {                // (eight products in a row that do not wait for one another)
+                Frag fk[4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    S[m][n] = M::mma(fk, w0[n], S[m][n]);
-                    if constexpr (sizeof(T) == 2) {
-                        S[m][n] = M::mma(fk, w1[n], S[m][n]);
-                        S[m][n] = M::mma(fk, w2[n], S[m][n]);
-                    }
-                }
+                for (int x = 0; x < 4; ++x) fk[x] = *(const Frag*)(ldskt + decay_operand<CROW>(xc, m + x, ks));
+#pragma unroll
+                for (int y = 0; y < W; ++y)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) S[m + x][n] = M::mma(fk[x], w[y][n], S[m + x][n]);
             }
         }
         __syncthreads();                                     // everything staged is read
@@ -545,7 +641,7 @@ __global__ __launch_bounds__(256, DK * DVT <= 128 * 128 ? 2 : 1) void decay_chun
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = decay_row<T>(m, 4 * lg + r), col = col0 + (wave * NT + n) * 16 + ln;
+                const int row = decay_row<T>(m, 4 * lg + r), col = col0 + decay_row<T>(wave * NT + n, ln);
                 if (row < p.dk && col < p.dv) dst[(size_t)row * p.dv + col] = S[m][n][r];
             }
     if (!OUT && tile == 0 && tid == 0) p.seg_factor[(size_t)bh * p.segments + seg] = make_float2(factor, cut);
@@ -614,19 +710,27 @@ static inline DecayPlan decay_plan(int dtype, int T, int B, int H, int dk, int d
     return q;
 }
 
-template <class T, int DK, int DVT>
+template <class T, int DK, int DVT, bool VEC>
 static hipError_t decay_launch_chunks(const DecayArgs& p, hipStream_t s)
 {
     const unsigned tiles = (p.dv + DVT - 1) / DVT, grid = (unsigned)((size_t)p.B * p.H * p.segments * tiles);
-    // (more than 64 KiB of LDS has to be asked for, once a kernel and device; asking again changes nothing)
     auto go = [&](auto out) -> hipError_t {
         constexpr bool OUT = decltype(out)::value;
         constexpr size_t lds = DecayLds<T, DK, DVT, OUT>::BYTES;
-        if constexpr (lds > 65536) {
-            hipError_t e = hipFuncSetAttribute((const void*)decay_chunk_kernel<T, DK, DVT, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const auto kernel = decay_chunk_kernel<T, DK, DVT, OUT, VEC>;
+        if constexpr (lds > 65536) {                         // has to be asked for, once a device
+            static std::atomic<uint64_t> asked{0};
+            int dev = 0;
+            hipError_t e = hipGetDevice(&dev);
             if (e != hipSuccess) return e;
+            const uint64_t bit = 1ull << (dev & 63);
+            if (dev > 63 || !(asked.load(std::memory_order_relaxed) & bit)) {
+                e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return e;
+                asked.fetch_or(bit, std::memory_order_relaxed);
+            }
         }
-        hipLaunchKernelGGL((decay_chunk_kernel<T, DK, DVT, OUT>), dim3(grid), dim3(256), lds, s, p);
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), lds, s, p);
         return hipSuccess;
     };
     if (p.segments > 1) {
@@ -640,10 +744,15 @@ static hipError_t decay_launch_chunks(const DecayArgs& p, hipStream_t s)
 template <class T>
 static hipError_t decay_launch(const DecayArgs& p, const DecayPlan& q, hipStream_t s)
 {
-    if (q.chunks) {
-        if (q.dk == 64) return q.dvt == 64 ? decay_launch_chunks<T, 64, 64>(p, s) : decay_launch_chunks<T, 64, 128>(p, s);
-        if (q.dk == 128) return q.dvt == 64 ? decay_launch_chunks<T, 128, 64>(p, s) : decay_launch_chunks<T, 128, 128>(p, s);
-        return decay_launch_chunks<T, 256, 64>(p, s);
+    if (q.chunks && p.vec_in) {
+        if (q.dk == 64) return q.dvt == 64 ? decay_launch_chunks<T, 64, 64, true>(p, s) : decay_launch_chunks<T, 64, 128, true>(p, s);
+        if (q.dk == 128) return q.dvt == 64 ? decay_launch_chunks<T, 128, 64, true>(p, s) : decay_launch_chunks<T, 128, 128, true>(p, s);
+        return decay_launch_chunks<T, 256, 64, true>(p, s);
+    }
+    if (q.chunks) {                                          // element by element: one width of columns is enough
+        if (q.dk == 64) return decay_launch_chunks<T, 64, 64, false>(p, s);
+        if (q.dk == 128) return decay_launch_chunks<T, 128, 64, false>(p, s);
+        return decay_launch_chunks<T, 256, 64, false>(p, s);
     }
     const unsigned grid = (unsigned)((size_t)p.B * p.H * ((p.dv + DECAY_COLS - 1) / DECAY_COLS));
     if (p.dk <= 64) hipLaunchKernelGGL((decay_recurrent_kernel<T, 64>), dim3(grid), dim3(256), 0, s, p);

@@ -145,8 +145,9 @@ extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, con
         return op_aligned(a, n * size) && dim % n == 0 && (d->steps == 1 || step % n == 0) && (d->rows == 1 || row % n == 0);
     };
     const int n16 = (int)(16 / size);
-    p.vec_q = whole(q, p.q_t, p.q_b, p.dk, n16); p.vec_k = whole(k, p.k_t, p.k_b, p.dk, n16); p.vec_v = whole(v, p.v_t, p.v_b, p.dv, n16);
-    p.vec_o = whole(out, p.o_t, p.o_b, p.dv, 4);
+    const int64_t near = ((int64_t)1 << 25) / (int64_t)size;
+    p.vec_in = whole(q, p.q_t, p.q_b, p.dk, n16) && whole(k, p.k_t, p.k_b, p.dk, n16) && whole(v, p.v_t, p.v_b, p.dv, n16) && p.q_t < near && p.k_t < near && p.v_t < near;
+    p.vec_o = whole(out, p.o_t, p.o_b, p.dv, n16);
     const hipError_t e = d->dtype == SEED_DTYPE_FP32 ? decay_launch<float>(p, plan, (hipStream_t)hip_stream) : decay_launch<__bf16>(p, plan, (hipStream_t)hip_stream);
     if (e != hipSuccess) return op_fail(SEED_ERR_DEVICE, "launch failed: %s", hipGetErrorString(e));
     return op_launched();
