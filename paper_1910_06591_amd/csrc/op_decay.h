@@ -458,8 +458,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                 const Frag fq = *(const Frag*)(ldsq + decay_operand<KROW>(xk, 0, d) + it * 16 * KROW);
 #pragma unroll
                 for (int x = 0; x < SC; ++x) {
-                    const int jt = IT == 4 ? x : wave & 1;
-                    if (jt <= it) sc[x] = M::mma(*(const Frag*)(ldsk + decay_operand<KROW>(xk, 0, d) + jt * 16 * KROW), fq, sc[x]);
+                    const int jt = IT == 4 ? x : wave & 1;   // (tiles above the diagonal too: the last wavefront needs all)
+                    sc[x] = M::mma(*(const Frag*)(ldsk + decay_operand<KROW>(xk, 0, d) + jt * 16 * KROW), fq, sc[x]);
                 }
             }
             __syncthreads();                                 // keys are read: scores take their place
@@ -475,7 +475,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int j = 16 * jt + 4 * lg + r;
-                        f[r] = j <= i && j >= low ? sc[x][r] * pw[j <= i ? i - j : 0] : 0.0f;
+                        const float w = pw[max(i - j, 0)] * sc[x][r];
+                        f[r] = j <= i && j >= low ? w : 0.0f;
                     }
                     if constexpr (sizeof(T) == 4) *(floatx4*)(ldsk + decay_at<CROW>(i, 4 * jt + lg)) = f;
                     else {
