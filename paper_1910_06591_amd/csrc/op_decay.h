@@ -222,7 +222,7 @@ template <class T, int DK, int DVT, bool OUT> struct DecayLds {
     static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (KROW > PARTS * CROW ? C * KROW : PARTS * C * CROW) : 0;
     // queries; keys, later the scores' parts; keys and values with their steps side by side; tables
     static constexpr int Q = 0, K = NQ, KT = K + NK, VT = KT + DK * CROW, END = VT + DVT * CROW;
-    static constexpr size_t BYTES = (size_t)END + (2 * C + 8) * sizeof(float) + 16;
+    static constexpr size_t BYTES = (size_t)END + (2 * C + 8) * sizeof(float) + 16 + (OUT ? (C + 4 + 512) * sizeof(float) : 0);
     static constexpr int RESIDENT = BYTES <= 80 * 1024 ? 2 : 1;          // workgroups a compute unit
 };
 
@@ -250,6 +250,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
     float* const pw = (float*)(decay_lds + L::END);          // powers 0 .. C
     float* const wend = pw + C + 4;                          // weight of step j in the state behind the chunk
     uint64_t* const flags = (uint64_t*)(wend + C + 4);       // [0]: steps with a flag, [1]: a value is not finite
+    float* const reach = (float*)(flags + 2);                // OUT: scale times power i + 1: what step i sees of the state
+    floatx4* const near = (floatx4*)(reach + C + 4);         // OUT: scale times the powers between a lane's steps of two tiles, see below
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 15, lg = lane >> 4;
     const int tiles = (p.dv + DVT - 1) / DVT;
@@ -272,6 +274,19 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
         double g = (double)p.decay[h], r = 1.0;
         for (int e = n; e; e >>= 1, g *= g) if (e & 1) r *= g;
         pw[n] = (float)r;
+        if (OUT && n > 0) reach[n - 1] = p.scale * (float)r;
+    }
+    if constexpr (OUT) {
+        // Lane: step ln of its tile, steps 4 lg .. of the other.  [0]: the same tile (zero above the diagonal); [1]: the
+        // tile in front of it; further ones by another power of 16 steps a tile.
+        __syncthreads();
+        if (wave == 0)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int n = ln - 4 * lg - r;
+                near[2 * lane][r] = n >= 0 ? p.scale * pw[n] : 0.0f;
+                near[2 * lane + 1][r] = p.scale * pw[16 + n];
+            }
     }
     const size_t state = (size_t)p.dk * p.dv;
     floatx4 S[MT][NT];
@@ -316,9 +331,10 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
             if constexpr (VEC) {
                 const uint32_t dd = min(d, dim - FE);
                 if (c == C) {
-                    const uint32_t off = (uint32_t)(j0 * step + dd) * (uint32_t)sizeof(T);
+                    const uint32_t one = (uint32_t)step * (uint32_t)sizeof(T);
+                    uint32_t off = (uint32_t)(j0 * step + dd) * (uint32_t)sizeof(T);
 #pragma unroll
-                    for (int j = 0; j < FE; ++j) blk[i][j] = *(const u32x4*)((const char*)(base + j * step) + off);
+                    for (int j = 0; j < FE; ++j, off += one) blk[i][j] = *(const u32x4*)((const char*)base + off);
                 } else
 #pragma unroll
                     for (int j = 0; j < FE; ++j) blk[i][j] = *(const u32x4*)((const char*)base + (uint32_t)(min(j0 + j, c - 1) * step + dd) * (uint32_t)sizeof(T));
@@ -466,18 +482,32 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
             if (nc > 0) fetch(next, nc);                     // on its way while the rest is multiplied
             {
                 const int i = 16 * it + ln;
-                const uint64_t upto = mask & ((2ull << i) - 1);
-                const int low = upto ? 63 - __builtin_clzll(upto) : 0;            // steps j from the last flag on
+                const floatx4 same = near[2 * lane], before = near[2 * lane + 1];
+                const float p16 = pw[16];
+                float far = 1.0f;                            // p16 ^ (it - jt - 1), from the nearest tile on
+#pragma unroll
+                for (int x = SC - 1; x >= 0; --x) {
+                    const int jt = IT == 4 ? x : wave & 1;
+                    if (jt > it) sc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    else if (jt == it) sc[x] *= same;
+                    else {
+                        sc[x] *= before * far;
+                        far *= p16;
+                    }
+                }
+                if (mask) {                                  // steps from the last flag on
+                    const uint64_t upto = mask & ((2ull << i) - 1);
+                    const int low = upto ? 63 - __builtin_clzll(upto) : 0;
+#pragma unroll
+                    for (int x = 0; x < SC; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (16 * (IT == 4 ? x : wave & 1) + 4 * lg + r < low) sc[x][r] = 0.0f;
+                }
 #pragma unroll
                 for (int x = 0; x < SC; ++x) {
                     const int jt = IT == 4 ? x : wave & 1;
-                    floatx4 f;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = 16 * jt + 4 * lg + r;
-                        const float w = pw[max(i - j, 0)] * sc[x][r];
-                        f[r] = j <= i && j >= low ? w : 0.0f;
-                    }
+                    const floatx4 f = sc[x];
                     if constexpr (sizeof(T) == 4) *(floatx4*)(ldsk + decay_at<CROW>(i, 4 * jt + lg)) = f;
                     else {
                         char* const to = ldsk + decay_at<CROW>(i, 2 * jt + (lg >> 1)) + 8 * (lg & 1);
@@ -523,7 +553,7 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
 #pragma unroll
             for (int it2 = 0; it2 < IT; ++it2) {
                 const int i = 16 * it2 + ln;
-                const float w = pw[i + 1];
+                const float w = reach[i];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[it2][n] *= w;
             }
@@ -565,14 +595,14 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                 if constexpr (sizeof(T) == 2 && NT == 2) {   // two tiles are eight consecutive columns
                     const int col = 32 * wave + 8 * lg;
                     if (p.vec_o && col + 8 <= dvt) {
-                        *(bf16x8*)(row + col) = to_bf16x8(acc[it2][0] * p.scale, acc[it2][1] * p.scale);
+                        *(bf16x8*)(row + col) = to_bf16x8(acc[it2][0], acc[it2][1]);
                         continue;
                     }
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const int col = decay_row<T>(wave * NT + n, 4 * lg);
-                    const floatx4 f = acc[it2][n] * p.scale;
+                    const floatx4 f = acc[it2][n];
                     if (p.vec_o && col + 4 <= dvt) {
                         if constexpr (sizeof(T) == 4) *(floatx4*)(row + col) = f;
                         else *(bf16x4*)(row + col) = to_bf16x4(f);
