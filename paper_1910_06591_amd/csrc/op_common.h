@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -23,6 +24,20 @@ __device__ __forceinline__ float op_activate(float x)
     if constexpr (ACT == SEED_ACT_RELU) return x < 0.0f ? 0.0f : x;    // (a comparison: NaN stays NaN)
     else if constexpr (ACT == SEED_ACT_SILU) return op_silu(x);
     else return x;
+}
+
+// More than 64 KiB of LDS has to be asked for, once a kernel and device; `asked` remembers the devices.
+static inline hipError_t op_allow_lds(const void* kernel, size_t bytes, std::atomic<uint64_t>& asked)
+{
+    if (bytes <= 65536) return hipSuccess;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (asked.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess && dev < 64) asked.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 static inline size_t op_dtype_size(int32_t dtype) { return dtype == SEED_DTYPE_FP32 ? 4 : 2; }

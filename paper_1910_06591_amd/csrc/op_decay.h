@@ -749,18 +749,9 @@ static hipError_t decay_launch_chunks(const DecayArgs& p, hipStream_t s)
         constexpr bool OUT = decltype(out)::value;
         constexpr size_t lds = DecayLds<T, DK, DVT, OUT>::BYTES;
         const auto kernel = decay_chunk_kernel<T, DK, DVT, OUT, VEC>;
-        if constexpr (lds > 65536) {                         // has to be asked for, once a device
-            static std::atomic<uint64_t> asked{0};
-            int dev = 0;
-            hipError_t e = hipGetDevice(&dev);
-            if (e != hipSuccess) return e;
-            const uint64_t bit = 1ull << (dev & 63);
-            if (dev > 63 || !(asked.load(std::memory_order_relaxed) & bit)) {
-                e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-                if (e != hipSuccess) return e;
-                asked.fetch_or(bit, std::memory_order_relaxed);
-            }
-        }
+        static std::atomic<uint64_t> asked{0};
+        const hipError_t e = op_allow_lds((const void*)kernel, lds, asked);
+        if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), lds, s, p);
         return hipSuccess;
     };

@@ -2,9 +2,18 @@
 //
 // The choices of a row are ordered by (logit descending, index ascending); every filter keeps a prefix of that order.
 // An element's place in it is a 64-bit key, the logit's bits in an order that integers have, then the inverted index:
-// larger key = earlier.  Masses exp((x - max) / T) are computed in 64 bits and added as 64-bit integers in units of
-// 2^-shift of the largest: a sum's value does not depend on the order of its terms, so neither does a choice.
+// larger key = earlier.  Masses are computed in 64 bits and added as 64-bit integers: a sum's value does not depend on
+// the order of its terms, so neither does a choice.  Kernels, by the number of choices (sample_launch):
+//   lanes  up to 64: a choice a lane, ranks by counting.
+//   row    a workgroup a row: one pass over the row adds every choice's mass to a histogram over the logit (2048 bins of
+//          1/16 of a temperature); what the filters and the draw ask for is then known up to a few bins; a second pass
+//          collects those bins' choices, which are sorted and searched.  The row is read twice, whatever the filters.
+//          Where the bins hold more choices than fit (logits that are all but equal), the questions are answered one
+//          by one instead, by radix searches over the row (sample_find).
 #pragma once
+#include <atomic>
+#include <type_traits>
+
 #include "op_common.h"
 
 namespace seedinf {
@@ -36,6 +45,114 @@ __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int off)
     return (uint64_t)hi << 32 | lo;
 }
 
+// exp on [0, 1/16], to 2^-54 of the value: Taylor's series; a is 16 times the argument
+__device__ __forceinline__ double sample_exp16(double a)
+{
+    double e = 1.0 / 40320 / 4294967296.0;                   // a^8 / (16^8 8!) ...
+    e = fma(e, a, 1.0 / 5040 / 268435456.0);
+    e = fma(e, a, 1.0 / 720 / 16777216.0);
+    e = fma(e, a, 1.0 / 120 / 1048576.0);
+    e = fma(e, a, 1.0 / 24 / 65536.0);
+    e = fma(e, a, 1.0 / 6 / 4096.0);
+    e = fma(e, a, 1.0 / 2 / 256.0);
+    e = fma(e, a, 1.0 / 16.0);
+    return fma(e, a, 1.0);
+}
+
+constexpr int SAMPLE_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BITS;
+
+// ---- reductions over a workgroup of NT threads; `scratch`: NT / 64 values ----
+template <int NT, class V, class F>
+__device__ __forceinline__ V sample_reduce(V v, V* scratch, F join)
+{
+    auto other = [](V x, int off) {
+        if constexpr (sizeof(V) == 8) { const uint64_t u = shfl_xor64(__builtin_bit_cast(uint64_t, x), off); return __builtin_bit_cast(V, u); }
+        else return __shfl_xor(x, off, 64);
+    };
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = join(v, other(v, off));
+    __syncthreads();                                         // the previous reduction's readers are done
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    V r = scratch[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) r = join(r, scratch[i]);
+    return r;
+}
+
+// Inclusive running sums of a[0 .. n) in place, n <= NT * PER, always added in the same order.
+template <int NT, int PER, class V>
+__device__ __forceinline__ void sample_scan(V* a, int n, V* scratch)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    V x[PER], s = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = tid * PER + i;
+        if (at < n) s += a[at];
+        x[i] = s;
+    }
+    V run = s;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const V o = __shfl_up(run, off, 64);
+        if (lane >= off) run += o;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[tid >> 6] = run;
+    __syncthreads();
+    V before = run - s;
+    if constexpr (sizeof(V) == 8) { before = __shfl_up(run, 1, 64); if (lane == 0) before = 0; }      // (double: a difference would round)
+    V waves = 0;
+    for (int w = 0; w < (tid >> 6); ++w) waves += scratch[w];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = tid * PER + i;
+        if (at < n) a[at] = waves + before + x[i];
+    }
+    __syncthreads();
+}
+
+// ---- a row of memory: 16-byte vectors between a head and a tail of single elements ----
+template <class T> struct SampleMem {
+    static constexpr int VEC = 16 / sizeof(T);
+    const T* x;
+    int V, head, vecs;
+    __device__ __forceinline__ SampleMem(const T* x_, int V_) : x(x_), V(V_)
+    {
+        head = min(V, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
+        vecs = (V - head) / VEC;
+    }
+    // f(value, index) for every element of tile `tile` (NT * U vectors; the head and the tail are tile 0's), in any order
+    template <int NT, int U, class F> __device__ __forceinline__ void tile(int tile, F f) const
+    {
+        const u32x4* body = (const u32x4*)(x + head);
+        const int first = tile * NT * U + (int)threadIdx.x;
+        u32x4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (first + u * NT < vecs) v[u] = body[first + u * NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u * NT < vecs) {
+                const int i = head + (first + u * NT) * VEC;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const uint32_t w = v[u][sizeof(T) == 4 ? e : e / 2];
+                    if constexpr (sizeof(T) == 4) f(__builtin_bit_cast(float, w), i + e);
+                    else f(e & 1 ? bf16_hi_f32(w) : bf16_lo_f32(w), i + e);
+                }
+            }
+        if (tile == 0) {
+            if ((int)threadIdx.x < head) f((float)x[threadIdx.x], (int)threadIdx.x);
+            const int i = head + vecs * VEC + (int)threadIdx.x;
+            if (i < V) f((float)x[i], i);
+        }
+    }
+    template <int NT, int U> __device__ __forceinline__ int tiles() const { return max(1, (vecs + NT * U - 1) / (NT * U)); }
+};
+
+// ---- radix searches: right for every row, several passes a question ----
+
 struct SampleRow {
     float top;                   // the largest logit
     double inv_t;
@@ -46,24 +163,21 @@ struct SampleRow {
     __device__ __forceinline__ uint64_t units(double m) const { return (uint64_t)(m * unit + 0.5); }
 };
 
-constexpr int SAMPLE_THREADS = 256;
-constexpr int SAMPLE_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BITS;
-
-// Radix search for one place of the order, from the largest key down, 11 bits of the key a pass: the first element
-// at which the running count reaches `count` (mass = false), or the running mass reaches (strict = false) or exceeds
-// (strict = true) `limit`.  Returns its key.  There has to be one.
-template <class T>
-__device__ uint64_t sample_find(const T* x, const SampleArgs& p, const SampleRow& row, bool mass, bool strict, uint64_t count, double limit,
-                                uint64_t* hist, uint64_t* share)
+// One place of the order, from the largest key down, 11 bits of the key a pass: the first element at which the running
+// count reaches `count` (mass = false), or the running mass reaches (strict = false) or exceeds (strict = true) `limit`.
+// Returns its key.  There has to be one.
+template <class T, int NT>
+__device__ __attribute__((noinline)) uint64_t sample_find(const T* x, int V, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
+                                                          uint64_t* hist, uint64_t* share)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, before = 0;
     int low = 64;                                            // key bits below `low` are not yet known
     while (low > 0) {
         const int w = low < SAMPLE_BITS ? low : SAMPLE_BITS, at = low - w;
-        for (int i = tid; i < SAMPLE_BINS; i += SAMPLE_THREADS) hist[i] = 0;
+        for (int i = tid; i < SAMPLE_BINS; i += NT) hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < p.V; i += SAMPLE_THREADS) {
+        for (int i = tid; i < V; i += NT) {
             const float f = sample_clean((float)x[i]);
             const uint64_t key = sample_key(f, i);
             if (low < 64 && (key >> low) != prefix) continue;
@@ -86,86 +200,384 @@ __device__ uint64_t sample_find(const T* x, const SampleArgs& p, const SampleRow
         prefix = prefix << w | share[0];
         before = share[1];
         low = at;
+        __syncthreads();
     }
     return prefix;
 }
 
-__device__ __forceinline__ uint64_t sample_block_sum(uint64_t v, uint64_t* scratch)
+// The filters and the draw of one row by such searches.  hist: SAMPLE_BINS values; best: the first key of the order.
+template <class T, int NT>
+__device__ __attribute__((noinline)) void sample_by_search(const SampleArgs& p, int r, const T* x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
+                                                           uint64_t* hist, uint64_t* scratch, uint64_t* share)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += shfl_xor64(v, off);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint64_t s = 0;
-    for (int i = 0; i < SAMPLE_THREADS / 64; ++i) s += scratch[i];
-    return s;
-}
-
-// One workgroup per row; every question about the order is a radix search over the row.
-template <class T>
-__global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs p)
-{
-    __shared__ uint64_t hist[SAMPLE_BINS];
-    __shared__ uint64_t scratch[SAMPLE_THREADS / 64];
-    __shared__ uint64_t share[2];
-    const int r = blockIdx.x, tid = threadIdx.x;
-    const T* x = (const T*)p.logits + (int64_t)r * p.stride;
-    // the first of the order
-    uint64_t best = 0;
-    for (int i = tid; i < p.V; i += SAMPLE_THREADS) {
-        const uint64_t key = sample_key(sample_clean((float)x[i]), i);
-        best = key > best ? key : best;
-    }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) { const uint64_t o = shfl_xor64(best, off); best = o > best ? o : best; }
-    if ((tid & 63) == 0) scratch[tid >> 6] = best;
-    __syncthreads();
-    for (int i = 0; i < SAMPLE_THREADS / 64; ++i) best = scratch[i] > best ? scratch[i] : best;
-    const int first = (int)~(uint32_t)best;
-    SampleRow row;
-    row.top = sample_clean((float)x[first]);
-    if (row.top == -INFINITY) {
-        if (tid == 0) { p.token[r] = -1; if (p.logprob) p.logprob[r] = -INFINITY; }
-        return;
-    }
-    const float temp = p.temperature ? p.temperature[r] : 1.0f;
-    if (!(temp > 0.0f)) {
-        if (tid == 0) { p.token[r] = first; if (p.logprob) p.logprob[r] = 0.0f; }
-        return;
-    }
-    row.inv_t = 1.0 / (double)temp;
-    row.unit = (double)(1ull << p.shift);
-    // the last kept key
-    uint64_t last = 0;
-    const int k = p.top_k ? p.top_k[r] : 0;
-    if (k > 0 && k < p.V) last = sample_find<T>(x, p, row, false, false, (uint64_t)k, 0.0, hist, share);
+    const int tid = threadIdx.x;
+    uint64_t last = 0;                                       // the last kept key
+    if (k > 0) last = sample_find<T, NT>(x, p.V, row, false, false, (uint64_t)k, 0.0, hist, share);
     auto total = [&](double least) {
         uint64_t s = 0;
-        for (int i = tid; i < p.V; i += SAMPLE_THREADS) {
+        for (int i = tid; i < p.V; i += NT) {
             const float f = sample_clean((float)x[i]);
             const uint64_t key = sample_key(f, i);
             if (key < last) continue;
             const double m = row.mass(f);
             if (m >= least || key == best) s += row.units(m);
         }
-        return sample_block_sum(s, scratch);
+        return sample_reduce<NT>(s, scratch, [](uint64_t a, uint64_t b) { return a + b; });
     };
-    const float top_p = p.top_p ? p.top_p[r] : 1.0f;
     if (top_p < 1.0f) {
         const double limit = (double)top_p * (double)total(0.0);
-        const uint64_t at = limit > 0.0 ? sample_find<T>(x, p, row, true, false, 0, limit, hist, share) : best;
+        const uint64_t at = limit > 0.0 ? sample_find<T, NT>(x, p.V, row, true, false, 0, limit, hist, share) : best;
         last = at > last ? at : last;
     }
-    const float min_p = p.min_p ? p.min_p[r] : 0.0f;
     const uint64_t z = total(min_p > 0.0f ? (double)min_p : 0.0);
-    float u = p.uniforms[r];
-    u = u > 0.0f ? (u < 1.0f ? u : 1.0f - 5.9604644775390625e-8f) : 0.0f;
-    const uint64_t at = sample_find<T>(x, p, row, true, true, 0, (double)u * (double)z, hist, share);
+    const uint64_t at = sample_find<T, NT>(x, p.V, row, true, true, 0, (double)u * (double)z, hist, share);
     if (tid == 0) {
-        const int i = (int)~(uint32_t)at;
+        const int i = min((int)(~(uint32_t)at & 0x7fffffffu), p.V - 1);
         p.token[r] = i;
         if (p.logprob) p.logprob[r] = (float)(row.exponent(sample_clean((float)x[i])) - log((double)z / row.unit));
+    }
+}
+
+// ---- a workgroup a row ----
+
+// The histogram's bins, from the first of the order on: u = 16 (16 - (x - centre) / T), bin floor(u).  Logits up to 16
+// temperatures above the centre and 112 below are in it; those further below have less than 2^-160 of the mass, which
+// is none; those above make the centre be chosen anew.  A choice's mass is that of its bin's lower edge, exp(16 -
+// (bin + 1) / 16) of the centre's, times exp((bin + 1 - u) / 16) in [1, 1.0645), in units of 2^-38: V up to 2^24 of
+// them stay below 2^63.
+struct SampleBins {
+    double inv_t, centre, B;     // B = 16 / T
+    __device__ __forceinline__ double place(float x) const { return fma(centre - (double)x, B, 256.0); }
+    // in units of 2^-38: rounded by adding 2^14, whose last place that is
+    __device__ __forceinline__ uint64_t units(double u, int bin) const
+    {
+        const double e = sample_exp16((double)(bin + 1) - u) + 16384.0;
+        return __builtin_bit_cast(uint64_t, e) - __builtin_bit_cast(uint64_t, 16384.0);
+    }
+    __device__ __forceinline__ static double edge(int bin) { return exp(16.0 - (bin + 1) * 0.0625) * (1.0 / 274877906944.0); }
+};
+
+template <int CAP> struct SampleLds {
+    uint64_t hist[SAMPLE_BINS];                              // masses; then, as doubles, their running sums
+    uint32_t count[SAMPLE_BINS];                             // choices; then their running sums
+    uint64_t list[CAP];                                      // keys of the collected choices
+    double run[CAP];                                         // running sums over them
+    uint32_t wanted[SAMPLE_BINS / 32];
+    uint64_t scratch[16], share[2];
+    int found, n;
+};
+
+template <class T, int NT, int CAP>
+__global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
+{
+    constexpr int U = 4, NB = SAMPLE_BINS;
+    extern __shared__ __attribute__((aligned(16))) char sample_lds[];
+    SampleLds<CAP>& l = *(SampleLds<CAP>*)sample_lds;
+    double* const cum = (double*)l.hist;
+    const int r = blockIdx.x, tid = threadIdx.x;
+    const SampleMem<T> row((const T*)p.logits + (int64_t)r * p.stride, p.V);
+    const float temp = p.temperature ? p.temperature[r] : 1.0f;
+    const int tiles = row.template tiles<NT, U>();
+    auto larger = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
+    auto first_key = [&](int from, int to) {                 // the first of the order among tiles from .. to
+        uint64_t best = 0;
+        for (int t = from; t < to; ++t) row.template tile<NT, U>(t, [&](float f, int i) { best = larger(best, sample_key(sample_clean(f), i)); });
+        return sample_reduce<NT>(best, l.scratch, larger);
+    };
+    auto value = [](uint64_t key) {                          // the logit of a key
+        const uint32_t b = (uint32_t)(key >> 32);
+        return __builtin_bit_cast(float, (b >> 31) ? b & 0x7fffffffu : ~b);
+    };
+    const int k0 = p.top_k ? p.top_k[r] : 0;
+    float min_p = p.min_p ? p.min_p[r] : 0.0f;
+    if (!(min_p > 0.0f)) min_p = 0.0f;
+    const bool greedy = !(temp > 0.0f) || k0 == 1 || min_p > 1.0f;       // one choice is kept
+    uint64_t best = first_key(0, greedy ? tiles : 1);
+    if (greedy) {
+        const bool none = value(best) == -INFINITY;
+        if (tid == 0) { p.token[r] = none ? -1 : (int)~(uint32_t)best; if (p.logprob) p.logprob[r] = none ? -INFINITY : 0.0f; }
+        return;
+    }
+    float top_p = p.top_p ? p.top_p[r] : 1.0f;
+    if (!(top_p < 1.0f)) top_p = 1.0f;
+    float u01 = p.uniforms[r];
+    u01 = u01 > 0.0f ? (u01 < 1.0f ? u01 : 1.0f - 5.9604644775390625e-8f) : 0.0f;
+    const int k = k0 > 0 && k0 < p.V ? k0 : 0;               // 0: off
+    const bool all_mass = top_p < 1.0f && k == 0;            // the mass of every choice is asked for
+
+    SampleBins bins;
+    bins.inv_t = 1.0 / (double)temp;
+    bins.B = 16.0 * bins.inv_t;
+    // Choices below `cut` (a logit, a little too low rather than too high) no longer matter.
+    float cut;
+    bool inf_row;                                            // +inf among the logits: those are the choices, all equal
+    for (int attempt = 0;; ++attempt) {
+        // the centre: the largest logit of the first tile; if one is found far above it, the largest of all
+        const float top = value(best);
+        inf_row = top == INFINITY;
+        if (top == -INFINITY && attempt > 0) {
+            if (tid == 0) { p.token[r] = -1; if (p.logprob) p.logprob[r] = -INFINITY; }
+            return;
+        }
+        bins.centre = inf_row || top == -INFINITY ? 0.0 : (double)top;
+        // min-p without top-p: nothing below it is asked for (the largest logit is not below the centre)
+        auto logit_at = [&](double u) {                      // (below the place's own logit by more than its roundings)
+            const double x = bins.centre + (256.0 - u) * 0.0625 * (double)temp;
+            return (float)(x - fabs(x) * 1e-6 - fabs(bins.centre) * 1e-6 - 1e-30);
+        };
+        cut = min_p > 0.0f && !all_mass && !(k && top_p < 1.0f) ? logit_at(257.0 - 16.0 * log((double)min_p)) : -INFINITY;
+        for (int i = tid; i < NB; i += NT) { l.hist[i] = 0; l.count[i] = 0; }
+        __syncthreads();
+        uint64_t seen = 0;
+        bool above = false;
+        for (int t = 0; t < tiles; ++t) {
+            row.template tile<NT, U>(t, [&](float f, int i) {
+                seen = larger(seen, sample_key(sample_clean(f), i));
+                if (f < cut) return;
+                if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
+                const double u = bins.place(f);
+                if (u < 0.0) above = true;
+                else if (u < (double)NB) {
+                    const int bin = (int)u;
+                    atomicAdd((unsigned long long*)&l.hist[bin], (unsigned long long)bins.units(u, bin));
+                    if (k) atomicAdd(&l.count[bin], 1u);
+                }
+            });
+            if (k && t == 0 && tiles > 2) {
+                // what is behind the k-th choice of one tile is behind the k-th of all
+                __syncthreads();
+                uint32_t mine = 0;
+                for (int i = tid * (NB / NT); i < (tid + 1) * (NB / NT); ++i) mine += l.count[i];
+                uint32_t run = mine;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) { const uint32_t o = __shfl_up(run, off, 64); if ((tid & 63) >= off) run += o; }
+                uint32_t* waves = (uint32_t*)l.scratch;
+                if (tid == 0) l.found = NB;
+                if ((tid & 63) == 63) waves[tid >> 6] = run;
+                __syncthreads();
+                for (int w = 0; w < (tid >> 6); ++w) run += waves[w];
+                if (run >= (uint32_t)k && run - mine < (uint32_t)k) l.found = (tid + 1) * (NB / NT);
+                __syncthreads();
+                if (l.found < NB) cut = fmaxf(cut, logit_at((double)l.found));
+                __syncthreads();
+            }
+        }
+        best = sample_reduce<NT>(seen, l.scratch, larger);
+        const uint64_t any = sample_reduce<NT>((uint64_t)above, l.scratch, larger);
+        if (!any && value(best) != -INFINITY && (value(best) == INFINITY) == inf_row && (top != -INFINITY || inf_row)) break;
+        if (attempt > 1) break;                              // (not reached: the second centre is the largest logit)
+    }
+    // running sums over the bins
+    for (int i = tid; i < NB; i += NT) { const uint64_t h = l.hist[i]; cum[i] = h ? (double)h * SampleBins::edge(i) : 0.0; }
+    __syncthreads();
+    sample_scan<NT, NB / NT>(cum, NB, (double*)l.scratch);
+    if (k) sample_scan<NT, NB / NT>(l.count, NB, (uint32_t*)l.scratch);
+    // the first bin whose running sum is ... ; NB - 1 if there is none
+    auto first_bin = [&](auto cond) {
+        __syncthreads();
+        if (tid == 0) l.found = NB - 1;
+        __syncthreads();
+        int at = NB - 1;
+#pragma unroll
+        for (int i = NB / NT - 1; i >= 0; --i) if (cond(tid * (NB / NT) + i)) at = tid * (NB / NT) + i;
+        if (at < NB - 1) atomicMin(&l.found, at);
+        __syncthreads();
+        return l.found;
+    };
+    auto before = [&](int b) { return b > 0 ? cum[b - 1] : 0.0; };
+    const double z_all = cum[NB - 1];
+    // The last kept choice lies in bin kb (top-k), between pb0 and pb1 (top-p), in mb (min-p); what is drawn between db0 and db1.
+    const bool k_on = k && l.count[NB - 1] >= (uint32_t)k;   // (choices that are in no bin have no mass)
+    const int kb = k_on ? first_bin([&](int b) { return l.count[b] >= (uint32_t)k; }) : NB - 1;
+    const bool k_part = k_on && l.count[kb] > (uint32_t)k;   // the bin is cut
+    const double zk0 = k_on ? before(kb) : z_all, zk1 = k_on ? cum[kb] : z_all;
+    int pb0 = NB - 1, pb1 = NB - 1;
+    if (top_p < 1.0f) {
+        const double t0 = (double)top_p * (k_part ? zk0 : zk1), t1 = (double)top_p * zk1;
+        pb0 = first_bin([&](int b) { return cum[b] >= t0 && cum[b] > 0.0; });
+        pb1 = first_bin([&](int b) { return cum[b] >= t1 && cum[b] > 0.0; });
+    }
+    const float top = value(best);
+    const double m_place = min_p > 0.0f ? bins.place(inf_row ? 0.0f : top) - 16.0 * log((double)min_p) : INFINITY;    // kept: u <= m_place
+    const int mb = m_place < (double)NB ? (int)fmax(m_place, 0.0) : NB - 1;
+    const int e0 = min(kb, min(pb0, mb)), e1 = min(kb, min(pb1, mb));
+    const double d0 = (double)u01 * before(e0), d1 = (double)u01 * cum[e1];
+    const int db0 = first_bin([&](int b) { return cum[b] > d0; }), db1 = first_bin([&](int b) { return cum[b] > d1; });
+    // collect the choices of those bins (and the first bin's, so that there is always one)
+    for (int i = tid; i < NB / 32; i += NT) l.wanted[i] = 0;
+    if (tid == 0) l.n = 0;
+    __syncthreads();
+    const int fb = min(max((int)bins.place(inf_row ? 0.0f : top), 0), NB - 1);
+    auto want = [&](int from, int to) { for (int b = from + tid; b <= to; b += NT) atomicOr(&l.wanted[b >> 5], 1u << (b & 31)); };
+    if (k_part) want(kb, kb);
+    if (top_p < 1.0f) want(pb0, pb1);
+    if (m_place < (double)NB) want(mb, mb);
+    want(db0, db1);
+    want(fb, fb);
+    __syncthreads();
+    int low = max(db1, fb);
+    if (k_part) low = max(low, kb);
+    if (top_p < 1.0f) low = max(low, pb1);
+    if (m_place < (double)NB) low = max(low, mb);
+    {
+        const double x = bins.centre + (255.0 - low) * 0.0625 * (double)temp;
+        cut = (float)(x - fabs(x) * 1e-6 - fabs(bins.centre) * 1e-6 - 1e-30);
+    }
+    for (int t = 0; t < tiles; ++t)
+        row.template tile<NT, U>(t, [&](float f, int i) {
+            if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
+            if (f < cut) return;
+            const double u = bins.place(f);
+            if (!(u < (double)NB) || !(u >= 0.0)) return;
+            const int bin = (int)u;
+            if (l.wanted[bin >> 5] >> (bin & 31) & 1) {
+                const int at = atomicAdd(&l.n, 1);
+                if (at < CAP) l.list[at] = sample_key(sample_clean(f), i);
+            }
+        });
+    __syncthreads();
+    const int n = l.n;
+    if (n > CAP) {                                           // (uniform)
+        SampleRow sr;
+        sr.top = top; sr.inv_t = bins.inv_t; sr.unit = (double)(1ull << p.shift);
+        __syncthreads();
+        sample_by_search<T, NT>(p, r, row.x, sr, best, k, top_p, min_p, u01, l.hist, l.scratch, l.share);
+        return;
+    }
+    // sort them, larger keys first (places behind n: key 0, behind all)
+    int size = 2;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += NT) l.list[i] = 0;
+    for (int a = 2; a <= size; a *= 2)
+        for (int b = a / 2; b > 0; b /= 2) {
+            __syncthreads();
+            for (int i = tid; i < size / 2; i += NT) {
+                const int x = 2 * i - (i & (b - 1)), y = x + b;
+                const uint64_t kx = l.list[x], ky = l.list[y];
+                if ((kx < ky) == ((x & a) == 0)) { l.list[x] = ky; l.list[y] = kx; }
+            }
+        }
+    __syncthreads();
+    // each one's mass; then the running sums over the list, and from them those over the whole order
+    auto place_of = [&](uint64_t key) { return bins.place(value(key)); };
+    for (int i = tid; i < n; i += NT) {
+        const double u = place_of(l.list[i]);
+        l.run[i] = (double)bins.units(u, (int)u) * SampleBins::edge((int)u);
+    }
+    __syncthreads();
+    sample_scan<NT, CAP / NT>(l.run, n, (double*)l.scratch);
+    // bin b's part of the list begins at starts(b) (its first element's place)
+    auto first_item = [&](int none, auto cond) {
+        __syncthreads();
+        if (tid == 0) l.found = none;
+        __syncthreads();
+        for (int i = tid; i < n; i += NT) if (cond(i)) { atomicMin(&l.found, i); break; }
+        __syncthreads();
+        return l.found;
+    };
+    auto bin_of = [&](int i) { return (int)place_of(l.list[i]); };
+    auto range = [&](int b, int& from, int& to) {            // [from, to): the list's part of bin b
+        from = first_item(n, [&](int i) { return bin_of(i) >= b; });
+        to = first_item(n, [&](int i) { return bin_of(i) > b; });
+    };
+    auto sum_at = [&](int i, int from, int b) { return before(b) + (l.run[i] - (from > 0 ? l.run[from - 1] : 0.0)); };
+    double z = z_all;                                        // mass of the kept ones
+    int end = NB;                                            // bin that the last kept one lies in
+    int f, t;
+    if (k_on) {
+        z = zk1; end = kb;
+        if (k_part) {
+            range(kb, f, t);
+            const int at = f + (int)((uint32_t)k - (kb > 0 ? l.count[kb - 1] : 0u)) - 1;
+            z = sum_at(at, f, kb);
+        }
+    }
+    if (top_p < 1.0f) {
+        const double limit = (double)top_p * z;
+        const int b = first_bin([&](int b) { return cum[b] >= limit && cum[b] > 0.0; });
+        range(b, f, t);
+        const int at = first_item(t - 1, [&](int i) { return i >= f && i < t && sum_at(i, f, b) >= limit; });
+        const double zp = f < t ? sum_at(at, f, b) : cum[b];
+        if (b < end || (b == end && zp < z)) { end = b; z = zp; }
+    }
+    if (m_place < (double)NB && mb <= end) {
+        range(mb, f, t);
+        const int at = first_item(t, [&](int i) { return i >= f && i < t && place_of(l.list[i]) > m_place; }) - 1;      // the last that is kept
+        const double zm = at >= f ? sum_at(at, f, mb) : before(mb);
+        if (mb < end || zm < z) { end = mb; z = zm; }
+    }
+    {                                                        // never fewer than one choice
+        const double one = l.run[0];                         // the list begins with the first of the order
+        if (!(z >= one)) z = one;
+    }
+    const double limit = (double)u01 * z;
+    const int b = first_bin([&](int b) { return cum[b] > limit; });
+    range(b, f, t);
+    const int at = first_item(max(t - 1, 0), [&](int i) { return i >= f && i < t && sum_at(i, f, b) > limit; });
+    if (tid == 0) {
+        const uint64_t key = l.list[at];
+        p.token[r] = (int)~(uint32_t)key;
+        if (p.logprob) {
+            const double u = place_of(key);
+            p.logprob[r] = (float)log((double)bins.units(u, (int)u) * SampleBins::edge((int)u) / z);
+        }
+    }
+}
+
+// ---- up to 64 choices: a choice a lane, L lanes a row ----
+template <class T, int L>
+__global__ __launch_bounds__(256) void sample_lanes_kernel(SampleArgs p)
+{
+    const int lane = threadIdx.x & 63, me = lane & (L - 1), base = lane & ~(L - 1);
+    const int r = blockIdx.x * (256 / L) + threadIdx.x / L;
+    const bool here = r < p.rows;                            // (every lane stays for the exchanges)
+    const float x = here && me < p.V ? sample_clean((float)((const T*)p.logits)[(int64_t)r * p.stride + me]) : -INFINITY;
+    const float temp = here ? (p.temperature ? p.temperature[r] : 1.0f) : 0.0f;
+    const int k0 = here && p.top_k ? p.top_k[r] : 0;
+    const float top_p = here && p.top_p ? p.top_p[r] : 1.0f, min_p = here && p.min_p ? p.min_p[r] : 0.0f;
+    float u = here ? p.uniforms[r] : 0.0f;
+    u = u > 0.0f ? (u < 1.0f ? u : 1.0f - 5.9604644775390625e-8f) : 0.0f;
+    // my place in the order
+    int rank = 0;
+    float top = -INFINITY;
+    for (int i = 0; i < p.V; ++i) {
+        const float o = __shfl(x, base + i, 64);
+        rank += o > x || (o == x && i < me);
+        top = fmaxf(top, o);
+    }
+    if (me >= p.V) rank = me;                                // (lanes without a choice: behind all)
+    const bool greedy = !(temp > 0.0f);
+    SampleRow row;
+    row.top = top; row.inv_t = greedy ? 1.0 : 1.0 / (double)temp; row.unit = 144115188075855872.0;      // 2^57
+    const double mine = x == -INFINITY ? 0.0 : row.mass(x);
+    // in the order: lane j of the row's has the j-th choice
+    auto push32 = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_permute((base + rank) * 4, (int)v); };
+    auto push64 = [&](uint64_t v) { return (uint64_t)push32((uint32_t)(v >> 32)) << 32 | push32((uint32_t)v); };
+    const int index = (int)push32((uint32_t)me);
+    const double m = __builtin_bit_cast(double, push64(__builtin_bit_cast(uint64_t, mine)));
+    const double ex = __builtin_bit_cast(double, push64(__builtin_bit_cast(uint64_t, row.exponent(x))));
+    uint64_t run = row.units(m);                             // running mass
+#pragma unroll
+    for (int off = 1; off < L; off <<= 1) {
+        const uint32_t lo = __shfl_up((int)(uint32_t)run, off, L), hi = __shfl_up((int)(uint32_t)(run >> 32), off, L);
+        if (me >= off) run += (uint64_t)hi << 32 | lo;
+    }
+    auto at = [&](uint64_t v, int i) { return (uint64_t)(uint32_t)__shfl((int)(uint32_t)(v >> 32), base + i, 64) << 32 | (uint32_t)__shfl((int)(uint32_t)v, base + i, 64); };
+    auto first = [&](bool c, int none) {                     // first lane of the row's with c
+        const uint64_t b = (__ballot(c) >> base) & (L == 64 ? ~0ull : (1ull << L) - 1);
+        return b ? (int)__builtin_ctzll(b) : none;
+    };
+    int n = greedy ? 1 : (k0 > 0 && k0 < p.V ? k0 : p.V);
+    if (top_p < 1.0f) n = min(n, 1 + first((double)run >= (double)top_p * (double)at(run, n - 1), n - 1));
+    if (min_p > 0.0f) n = min(n, max(1, first(!(m >= (double)min_p), L)));
+    const uint64_t z = at(run, n - 1);
+    const int drawn = first((double)run > (double)u * (double)z, n - 1);
+    const int token = __shfl(index, base + drawn, 64);
+    const double e = __builtin_bit_cast(double, at(__builtin_bit_cast(uint64_t, ex), drawn));
+    if (here && me == 0) {
+        const bool none = top == -INFINITY;
+        p.token[r] = none ? -1 : token;
+        if (p.logprob) p.logprob[r] = none ? -INFINITY : greedy ? 0.0f : (float)(e - log((double)z / row.unit));
     }
 }
 
@@ -176,10 +588,32 @@ static inline int sample_shift(int V)
     return 62 - bits < 52 ? 62 - bits : 52;
 }
 
+constexpr int SAMPLE_SMALL = 8192;       // choices up to which a row is 256 threads' work
+
 template <class T>
-static void sample_launch(const SampleArgs& p, hipStream_t s)
+static hipError_t sample_launch(const SampleArgs& p, hipStream_t s)
 {
-    hipLaunchKernelGGL((sample_kernel<T>), dim3((unsigned)p.rows), dim3(SAMPLE_THREADS), 0, s, p);
+    if (p.V <= 64) {
+        auto go = [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            hipLaunchKernelGGL((sample_lanes_kernel<T, L>), dim3((unsigned)((p.rows + 256 / L - 1) / (256 / L))), dim3(256), 0, s, p);
+        };
+        if (p.V <= 8) go(std::integral_constant<int, 8>{});
+        else if (p.V <= 16) go(std::integral_constant<int, 16>{});
+        else if (p.V <= 32) go(std::integral_constant<int, 32>{});
+        else go(std::integral_constant<int, 64>{});
+        return hipSuccess;
+    }
+    if (p.V <= SAMPLE_SMALL) {
+        hipLaunchKernelGGL((sample_row_kernel<T, 256, 1024>), dim3((unsigned)p.rows), dim3(256), sizeof(SampleLds<1024>), s, p);
+        return hipSuccess;
+    }
+    constexpr size_t lds = sizeof(SampleLds<4096>);
+    static std::atomic<uint64_t> asked{0};
+    const hipError_t e = op_allow_lds((const void*)sample_row_kernel<T, 1024, 4096>, lds, asked);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((sample_row_kernel<T, 1024, 4096>), dim3((unsigned)p.rows), dim3(1024), lds, s, p);
+    return hipSuccess;
 }
 
 }  // namespace seedinf
