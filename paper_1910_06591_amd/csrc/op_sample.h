@@ -167,7 +167,7 @@ struct SampleRow {
 // count reaches `count` (mass = false), or the running mass reaches (strict = false) or exceeds (strict = true) `limit`.
 // Returns its key.  There has to be one.
 template <class T, int NT>
-__device__ __attribute__((noinline)) uint64_t sample_find(const T* x, int V, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
+__device__ __forceinline__ uint64_t sample_find(const T* x, int V, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
                                                           uint64_t* hist, uint64_t* share)
 {
     const int tid = threadIdx.x;
@@ -207,7 +207,7 @@ __device__ __attribute__((noinline)) uint64_t sample_find(const T* x, int V, Sam
 
 // The filters and the draw of one row by such searches.  hist: SAMPLE_BINS values; best: the first key of the order.
 template <class T, int NT>
-__device__ __attribute__((noinline)) void sample_by_search(const SampleArgs& p, int r, const T* x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
+__device__ __forceinline__ void sample_by_search(const SampleArgs& p, int r, const T* x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
                                                            uint64_t* hist, uint64_t* scratch, uint64_t* share)
 {
     const int tid = threadIdx.x;
@@ -279,11 +279,12 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     const float temp = p.temperature ? p.temperature[r] : 1.0f;
     const int tiles = row.template tiles<NT, U>();
     auto larger = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
-    auto first_key = [&](int from, int to) {                 // the first of the order among tiles from .. to
+    auto first_key = [&]() {                                 // the first of the order
         uint64_t best = 0;
-        for (int t = from; t < to; ++t) row.template tile<NT, U>(t, [&](float f, int i) { best = larger(best, sample_key(sample_clean(f), i)); });
+        for (int t = 0; t < tiles; ++t) row.template tile<NT, U>(t, [&](float f, int i) { best = larger(best, sample_key(sample_clean(f), i)); });
         return sample_reduce<NT>(best, l.scratch, larger);
     };
+    auto largest = [&](float f) { return sample_reduce<NT>(f, (float*)l.scratch, [](float a, float b) { return fmaxf(a, b); }); };
     auto value = [](uint64_t key) {                          // the logit of a key
         const uint32_t b = (uint32_t)(key >> 32);
         return __builtin_bit_cast(float, (b >> 31) ? b & 0x7fffffffu : ~b);
@@ -292,8 +293,8 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     float min_p = p.min_p ? p.min_p[r] : 0.0f;
     if (!(min_p > 0.0f)) min_p = 0.0f;
     const bool greedy = !(temp > 0.0f) || k0 == 1 || min_p > 1.0f;       // one choice is kept
-    uint64_t best = first_key(0, greedy ? tiles : 1);
     if (greedy) {
+        const uint64_t best = first_key();
         const bool none = value(best) == -INFINITY;
         if (tid == 0) { p.token[r] = none ? -1 : (int)~(uint32_t)best; if (p.logprob) p.logprob[r] = none ? -INFINITY : 0.0f; }
         return;
@@ -310,12 +311,14 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     bins.B = 16.0 * bins.inv_t;
     // Choices below `cut` (a logit, a little too low rather than too high) no longer matter.
     float cut;
+    float top = -INFINITY;                                   // the largest logit, as far as it is known (NaN is none: fmaxf)
+    row.template tile<NT, U>(0, [&](float f, int) { top = fmaxf(top, f); });
+    top = largest(top);
     bool inf_row;                                            // +inf among the logits: those are the choices, all equal
     for (int attempt = 0;; ++attempt) {
         // the centre: the largest logit of the first tile; if one is found far above it, the largest of all
-        const float top = value(best);
         inf_row = top == INFINITY;
-        if (top == -INFINITY && attempt > 0) {
+        if (top == -INFINITY && attempt > 0) {               // no choice at all
             if (tid == 0) { p.token[r] = -1; if (p.logprob) p.logprob[r] = -INFINITY; }
             return;
         }
@@ -328,17 +331,15 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         cut = min_p > 0.0f && !all_mass && !(k && top_p < 1.0f) ? logit_at(257.0 - 16.0 * log((double)min_p)) : -INFINITY;
         for (int i = tid; i < NB; i += NT) { l.hist[i] = 0; l.count[i] = 0; }
         __syncthreads();
-        uint64_t seen = 0;
-        bool above = false;
+        float seen = -INFINITY;
         for (int t = 0; t < tiles; ++t) {
             row.template tile<NT, U>(t, [&](float f, int i) {
-                seen = larger(seen, sample_key(sample_clean(f), i));
-                if (f < cut) return;
+                seen = fmaxf(seen, f);
+                if (!(f >= cut)) return;                     // (NaN neither)
                 if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
                 const double u = bins.place(f);
-                if (u < 0.0) above = true;
-                else if (u < (double)NB) {
-                    const int bin = (int)u;
+                const int bin = (int)floor(u);               // (saturates; a NaN, of -inf at an infinite temperature, is not in [0, NB) below)
+                if ((unsigned)bin < (unsigned)NB && u >= 0.0) {
                     atomicAdd((unsigned long long*)&l.hist[bin], (unsigned long long)bins.units(u, bin));
                     if (k) atomicAdd(&l.count[bin], 1u);
                 }
@@ -362,10 +363,10 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
                 __syncthreads();
             }
         }
-        best = sample_reduce<NT>(seen, l.scratch, larger);
-        const uint64_t any = sample_reduce<NT>((uint64_t)above, l.scratch, larger);
-        if (!any && value(best) != -INFINITY && (value(best) == INFINITY) == inf_row && (top != -INFINITY || inf_row)) break;
-        if (attempt > 1) break;                              // (not reached: the second centre is the largest logit)
+        const float was = top;
+        top = largest(seen);
+        // nothing lies above the bins (and the centre was a logit, the row of the kind that was assumed)
+        if (attempt > 0 ? top != -INFINITY : was != -INFINITY && (top == INFINITY) == inf_row && (inf_row || bins.place(top) >= 0.0)) break;
     }
     // running sums over the bins
     for (int i = tid; i < NB; i += NT) { const uint64_t h = l.hist[i]; cum[i] = h ? (double)h * SampleBins::edge(i) : 0.0; }
@@ -380,7 +381,8 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         int at = NB - 1;
 #pragma unroll
         for (int i = NB / NT - 1; i >= 0; --i) if (cond(tid * (NB / NT) + i)) at = tid * (NB / NT) + i;
-        if (at < NB - 1) atomicMin(&l.found, at);
+        const uint64_t some = __ballot(at < NB - 1);         // (the first lane's is the wavefront's first)
+        if (some && (tid & 63) == (int)__builtin_ctzll(some)) atomicMin(&l.found, at);
         __syncthreads();
         return l.found;
     };
@@ -397,7 +399,6 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         pb0 = first_bin([&](int b) { return cum[b] >= t0 && cum[b] > 0.0; });
         pb1 = first_bin([&](int b) { return cum[b] >= t1 && cum[b] > 0.0; });
     }
-    const float top = value(best);
     const double m_place = min_p > 0.0f ? bins.place(inf_row ? 0.0f : top) - 16.0 * log((double)min_p) : INFINITY;    // kept: u <= m_place
     const int mb = m_place < (double)NB ? (int)fmax(m_place, 0.0) : NB - 1;
     const int e0 = min(kb, min(pb0, mb)), e1 = min(kb, min(pb1, mb));
@@ -441,22 +442,39 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         SampleRow sr;
         sr.top = top; sr.inv_t = bins.inv_t; sr.unit = (double)(1ull << p.shift);
         __syncthreads();
+        const uint64_t best = first_key();
         sample_by_search<T, NT>(p, r, row.x, sr, best, k, top_p, min_p, u01, l.hist, l.scratch, l.share);
         return;
     }
-    // sort them, larger keys first (places behind n: key 0, behind all)
-    int size = 2;
-    while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += NT) l.list[i] = 0;
-    for (int a = 2; a <= size; a *= 2)
-        for (int b = a / 2; b > 0; b /= 2) {
-            __syncthreads();
-            for (int i = tid; i < size / 2; i += NT) {
-                const int x = 2 * i - (i & (b - 1)), y = x + b;
-                const uint64_t kx = l.list[x], ky = l.list[y];
-                if ((kx < ky) == ((x & a) == 0)) { l.list[x] = ky; l.list[y] = kx; }
-            }
+    // sort them, larger keys first: few by counting those in front of each, many by a bitonic network (places behind n
+    // there: key 0, behind all)
+    if (n <= 1024) {
+        uint64_t mine[1024 / NT];
+        int rank[1024 / NT];
+#pragma unroll
+        for (int j = 0; j < 1024 / NT; ++j) { mine[j] = tid + j * NT < n ? l.list[tid + j * NT] : 0; rank[j] = 0; }
+        for (int i = 0; i < n; ++i) {
+            const uint64_t key = l.list[i];
+#pragma unroll
+            for (int j = 0; j < 1024 / NT; ++j) rank[j] += key > mine[j];
         }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 1024 / NT; ++j) if (tid + j * NT < n) l.list[rank[j]] = mine[j];
+    } else {
+        int size = 2048;
+        while (size < n) size *= 2;
+        for (int i = n + tid; i < size; i += NT) l.list[i] = 0;
+        for (int a = 2; a <= size; a *= 2)
+            for (int b = a / 2; b > 0; b /= 2) {
+                __syncthreads();
+                for (int i = tid; i < size / 2; i += NT) {
+                    const int x = 2 * i - (i & (b - 1)), y = x + b;
+                    const uint64_t kx = l.list[x], ky = l.list[y];
+                    if ((kx < ky) == ((x & a) == 0)) { l.list[x] = ky; l.list[y] = kx; }
+                }
+            }
+    }
     __syncthreads();
     // each one's mass; then the running sums over the list, and from them those over the whole order
     auto place_of = [&](uint64_t key) { return bins.place(value(key)); };
@@ -471,7 +489,14 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         __syncthreads();
         if (tid == 0) l.found = none;
         __syncthreads();
-        for (int i = tid; i < n; i += NT) if (cond(i)) { atomicMin(&l.found, i); break; }
+        int mine = none;
+        for (int i = tid; i < n; i += NT) if (cond(i)) { mine = i; break; }
+        const uint64_t some = __ballot(mine < none);         // (in front of `none`, the first lane's is the wavefront's first of its round)
+        if (some) {
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) mine = min(mine, __shfl_xor(mine, off, 64));
+            if ((tid & 63) == 0) atomicMin(&l.found, mine);
+        }
         __syncthreads();
         return l.found;
     };
