@@ -7,11 +7,13 @@
 //   lanes  up to 64: a choice a lane, ranks by counting.
 //   row    a workgroup a row: one pass over the row adds every choice's mass to a histogram over the logit (2048 bins of
 //          1/16 of a temperature); what the filters and the draw ask for is then known up to a few bins; a second pass
-//          collects those bins' choices, which are sorted and searched.  The row is read twice, whatever the filters.
+//          collects those bins' choices, which are sorted and searched.  A row that top-k or min-p leaves few choices
+//          is read once: those go into a list that takes the row's place.
 //          Where the bins hold more choices than fit (logits that are all but equal), the questions are answered one
 //          by one instead, by radix searches over the row (sample_find).
 #pragma once
 #include <atomic>
+#include <cfloat>
 #include <type_traits>
 
 #include "op_common.h"
@@ -314,8 +316,108 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     float top = -INFINITY;                                   // the largest logit, as far as it is known (NaN is none: fmaxf)
     row.template tile<NT, U>(0, [&](float f, int) { top = fmaxf(top, f); });
     top = largest(top);
-    bool inf_row;                                            // +inf among the logits: those are the choices, all equal
-    for (int attempt = 0;; ++attempt) {
+    bool inf_row = top == INFINITY;                          // +inf among the logits: those are the choices, all equal
+    // (below the place's own logit by more than its roundings)
+    auto logit_at = [&](double u) {
+        const double x = bins.centre + (256.0 - u) * 0.0625 * (double)temp;
+        return (float)(x - fabs(x) * 1e-6 - fabs(bins.centre) * 1e-6 - 1e-30);
+    };
+    // The end of the bins up to which the first k choices counted in l.count lie, NB if there are not as many.
+    auto k_end = [&]() {
+        __syncthreads();
+        uint32_t mine = 0;
+        for (int i = tid * (NB / NT); i < (tid + 1) * (NB / NT); ++i) mine += l.count[i];
+        uint32_t run = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) { const uint32_t o = __shfl_up(run, off, 64); if ((tid & 63) >= off) run += o; }
+        uint32_t* waves = (uint32_t*)l.scratch;
+        if (tid == 0) l.found = NB;
+        if ((tid & 63) == 63) waves[tid >> 6] = run;
+        __syncthreads();
+        for (int w = 0; w < (tid >> 6); ++w) run += waves[w];
+        if (run >= (uint32_t)k && run - mine < (uint32_t)k) l.found = (tid + 1) * (NB / NT);
+        __syncthreads();
+        return l.found;
+    };
+    auto clear = [&]() {
+        __syncthreads();
+        for (int i = tid; i < NB; i += NT) { l.hist[i] = 0; l.count[i] = 0; }
+        __syncthreads();
+    };
+    auto bin_at = [&](double u) { return (unsigned)(int)floor(u) < (unsigned)NB && u >= 0.0 ? (int)u : -1; };        // (NaN: none)
+    auto add = [&](float f) {                                // a choice to the histogram
+        const double u = bins.place(f);
+        const int bin = bin_at(u);
+        if (bin >= 0) {
+            atomicAdd((unsigned long long*)&l.hist[bin], (unsigned long long)bins.units(u, bin));
+            if (k) atomicAdd(&l.count[bin], 1u);
+        }
+    };
+    // Where a filter leaves few choices whatever the rest of the row, the row is read once and those that may be among
+    // them are kept in a list: all that are not behind the k-th, or not below min-p, of what was read so far.  The mass of
+    // the others is not asked for.  If the list does not hold them, the row is taken as a whole below.
+    uint64_t* const cand = (uint64_t*)l.run;
+    int cands = 0;
+    bool listed = tiles > 1 && !inf_row && top != -INFINITY && (k ? k <= CAP / 2 : min_p > 0.0f && !all_mass);
+    if (listed) {
+        bins.centre = (double)top;
+        cut = -FLT_MAX;
+        auto narrow = [&]() {                                // the cut, from the counts (k) or the largest logit (min-p)
+            if (k) { const int e = k_end(); if (e < NB) cut = fmaxf(cut, logit_at((double)e)); }
+            if (min_p > 0.0f && (k == 0 || !(top_p < 1.0f))) cut = fmaxf(cut, logit_at(257.0 - 16.0 * log((double)min_p)));
+        };
+        if (k) {
+            clear();
+            row.template tile<NT, U>(0, [&](float f, int) { const int bin = bin_at(bins.place(f)); if (bin >= 0) atomicAdd(&l.count[bin], 1u); });
+        }
+        narrow();
+        __syncthreads();
+        if (tid == 0) l.n = 0;
+        __syncthreads();
+        for (int t = 0; t < tiles; ++t) {
+            row.template tile<NT, U>(t, [&](float f, int i) {
+                if (f >= cut) {
+                    const int at = atomicAdd(&l.n, 1);
+                    if (at < CAP) cand[at] = sample_key(f + 0.0f, i);
+                }
+            });
+            __syncthreads();
+            cands = l.n;
+            if (cands > CAP) break;
+            if (cands > CAP / 2 || t == tiles - 1) {         // the centre at the largest so far, the cut anew, and out with what is below it
+                uint64_t mine[CAP / NT];
+                top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < CAP / NT; ++j) {
+                    mine[j] = tid + j * NT < cands ? cand[tid + j * NT] : 0;
+                    if (mine[j]) top = fmaxf(top, value(mine[j]));
+                }
+                top = largest(top);
+                if (top == INFINITY) break;
+                bins.centre = (double)top;
+                clear();
+                if (k)
+#pragma unroll
+                    for (int j = 0; j < CAP / NT; ++j)
+                        if (mine[j]) { const int bin = bin_at(bins.place(value(mine[j]))); if (bin >= 0) atomicAdd(&l.count[bin], 1u); }
+                narrow();
+                __syncthreads();
+                if (tid == 0) l.n = 0;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < CAP / NT; ++j) if (mine[j] && value(mine[j]) >= cut) cand[atomicAdd(&l.n, 1)] = mine[j];
+                __syncthreads();
+                cands = l.n;
+            }
+        }
+        listed = cands <= CAP && top != INFINITY;
+        if (listed) {
+            clear();
+            for (int i = tid; i < cands; i += NT) add(value(cand[i]));
+        }
+        __syncthreads();
+    }
+    for (int attempt = 0; !listed; ++attempt) {
         // the centre: the largest logit of the first tile; if one is found far above it, the largest of all
         inf_row = top == INFINITY;
         if (top == -INFINITY && attempt > 0) {               // no choice at all
@@ -324,42 +426,20 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         }
         bins.centre = inf_row || top == -INFINITY ? 0.0 : (double)top;
         // min-p without top-p: nothing below it is asked for (the largest logit is not below the centre)
-        auto logit_at = [&](double u) {                      // (below the place's own logit by more than its roundings)
-            const double x = bins.centre + (256.0 - u) * 0.0625 * (double)temp;
-            return (float)(x - fabs(x) * 1e-6 - fabs(bins.centre) * 1e-6 - 1e-30);
-        };
         cut = min_p > 0.0f && !all_mass && !(k && top_p < 1.0f) ? logit_at(257.0 - 16.0 * log((double)min_p)) : -INFINITY;
-        for (int i = tid; i < NB; i += NT) { l.hist[i] = 0; l.count[i] = 0; }
-        __syncthreads();
+        clear();
         float seen = -INFINITY;
         for (int t = 0; t < tiles; ++t) {
             row.template tile<NT, U>(t, [&](float f, int i) {
                 seen = fmaxf(seen, f);
                 if (!(f >= cut)) return;                     // (NaN neither)
                 if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
-                const double u = bins.place(f);
-                const int bin = (int)floor(u);               // (saturates; a NaN, of -inf at an infinite temperature, is not in [0, NB) below)
-                if ((unsigned)bin < (unsigned)NB && u >= 0.0) {
-                    atomicAdd((unsigned long long*)&l.hist[bin], (unsigned long long)bins.units(u, bin));
-                    if (k) atomicAdd(&l.count[bin], 1u);
-                }
+                add(f);
             });
+            // what is behind the k-th choice of one tile is behind the k-th of all
             if (k && t == 0 && tiles > 2) {
-                // what is behind the k-th choice of one tile is behind the k-th of all
-                __syncthreads();
-                uint32_t mine = 0;
-                for (int i = tid * (NB / NT); i < (tid + 1) * (NB / NT); ++i) mine += l.count[i];
-                uint32_t run = mine;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) { const uint32_t o = __shfl_up(run, off, 64); if ((tid & 63) >= off) run += o; }
-                uint32_t* waves = (uint32_t*)l.scratch;
-                if (tid == 0) l.found = NB;
-                if ((tid & 63) == 63) waves[tid >> 6] = run;
-                __syncthreads();
-                for (int w = 0; w < (tid >> 6); ++w) run += waves[w];
-                if (run >= (uint32_t)k && run - mine < (uint32_t)k) l.found = (tid + 1) * (NB / NT);
-                __syncthreads();
-                if (l.found < NB) cut = fmaxf(cut, logit_at((double)l.found));
+                const int e = k_end();
+                if (e < NB) cut = fmaxf(cut, logit_at((double)e));
                 __syncthreads();
             }
         }
@@ -424,18 +504,21 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         const double x = bins.centre + (255.0 - low) * 0.0625 * (double)temp;
         cut = (float)(x - fabs(x) * 1e-6 - fabs(bins.centre) * 1e-6 - 1e-30);
     }
-    for (int t = 0; t < tiles; ++t)
-        row.template tile<NT, U>(t, [&](float f, int i) {
-            if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
-            if (f < cut) return;
-            const double u = bins.place(f);
-            if (!(u < (double)NB) || !(u >= 0.0)) return;
-            const int bin = (int)u;
-            if (l.wanted[bin >> 5] >> (bin & 31) & 1) {
-                const int at = atomicAdd(&l.n, 1);
-                if (at < CAP) l.list[at] = sample_key(sample_clean(f), i);
-            }
-        });
+    auto collect = [&](float f, int i) {
+        const int bin = bin_at(bins.place(f));
+        if (bin >= 0 && (l.wanted[bin >> 5] >> (bin & 31) & 1)) {
+            const int at = atomicAdd(&l.n, 1);
+            if (at < CAP) l.list[at] = sample_key(f + 0.0f, i);
+        }
+    };
+    if (listed)
+        for (int i = tid; i < cands; i += NT) collect(value(cand[i]), (int)~(uint32_t)cand[i]);
+    else
+        for (int t = 0; t < tiles; ++t)
+            row.template tile<NT, U>(t, [&](float f, int i) {
+                if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
+                if (f >= cut) collect(f, i);
+            });
     __syncthreads();
     const int n = l.n;
     if (n > CAP) {                                           // (uniform)
