@@ -7,6 +7,8 @@ fallback: if the shared library is missing or a call fails, this raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import math
 import os
 import subprocess
 
@@ -512,34 +514,34 @@ def _op_arg(t, dtype, shape, name, device):
     return t.data_ptr()
 
 
-class _OpCall:
-    """The device and stream of one operator call.  Memory allocated inside belongs to that stream: a workspace goes
-    back to torch's allocator behind the kernels that use it, whichever stream that is."""
+@functools.lru_cache(maxsize=1)
+def _raw_calls():
+    """(current device, current stream's handle on a device): torch's own calls without the objects it wraps round them,
+    which cost a small operator a quarter of its time on the host; the public calls where a torch has no such ones."""
+    import torch
+    device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return device, handle
 
-    def __init__(self, device, stream):
-        import torch
-        self.device, self.stream = device, stream
-        self.guards = []
-        if device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(device))
-        if stream is not None:
-            self.guards.append(torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)))
 
-    def __enter__(self):
-        import torch
-        for g in self.guards:
-            g.__enter__()
-        if self.stream is None:
-            self.stream = torch.cuda.current_stream(self.device).cuda_stream
-        return self
+def _on_stream(device, stream, call):
+    """call(stream handle) with `device` current.  A stream of the caller's is made the current one for the call: what is
+    allocated inside, a workspace above all, then goes back to torch's allocator behind that stream's kernels."""
+    import torch
+    if stream is None:
+        current, handle = _raw_calls()
+        if device.index == current():
+            return call(handle(device.index))
+        with torch.cuda.device(device):
+            return call(handle(device.index))
+    theirs = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(theirs):
+        return call(stream)
 
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
 
-    def workspace(self, n):
-        import torch
-        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+def _op_workspace(n, device):
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
 def _op_check(lib, st):
@@ -547,14 +549,59 @@ def _op_check(lib, st):
         raise SeedError(st, lib.seed_op_last_error().decode())
 
 
+# What follows from sizes and strides alone is kept by them: descriptors and workspace sizes.
+@functools.lru_cache(maxsize=1024)
+def _decay_desc(*fields):
+    d = SeedDecay(C.sizeof(SeedDecay), *fields)
+    return d, C.addressof(d), int(load_library().seed_op_decay_workspace(C.addressof(d)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(*sizes):
+    return int(load_library().seed_op_group_norm_workspace(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _sample_workspace(*sizes):
+    return int(load_library().seed_op_sample_workspace(*sizes))
+
+
 def _strided(t, shape, name, dtype, device):
-    """A [steps, rows, heads, dim] tensor whose heads are dense in a row: its address and the strides of a step and a row."""
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
-        raise TypeError(f"{name} must be {dtype} of shape {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    """A [..., rows, heads, dim] tensor whose heads are dense in a row: its address and the strides in front of them."""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        raise TypeError(f"{name} must be {dtype} of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     st = t.stride()
-    if t.numel() and ((shape[3] > 1 and st[3] != 1) or (shape[2] > 1 and st[2] != shape[3])):
+    if (st[-1] != 1 and shape[-1] > 1 or st[-2] != shape[-1] and shape[-2] > 1) and t.numel():
         raise TypeError(f"{name}: a row's heads must be dense, got strides {st}")
-    return t.data_ptr(), st[0], st[1]
+    return (t.data_ptr(), *st[:-2]) if len(st) == 4 else (t.data_ptr(), 0, st[0])
+
+
+def _decay(front, q, k, v, decay, state, done, lengths, scale, out, state_out, stream):
+    """front: the sizes in front of [heads, dim]: (steps, rows), or (rows,) for one step."""
+    import torch
+    lib = load_library()
+    dt, dev, dtype = _op_dtype(q, "q"), q.device, q.dtype
+    B, (H, dk), KV, dv = front[-1], q.shape[-2:], k.shape[-2], v.shape[-1]
+
+    def call(handle):
+        o = out
+        if o is None:
+            o = (torch.empty if lengths is None else torch.zeros)((*front, H, dv), dtype=dtype, device=dev)
+        so = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev) if state_out is None else state_out
+        pq, q0, q1 = _strided(q, (*front, H, dk), "q", dtype, dev)
+        pk, k0, k1 = _strided(k, (*front, KV, dk), "k", dtype, dev)
+        pv, v0, v1 = _strided(v, (*front, KV, dv), "v", dtype, dev)
+        po, o0, o1 = _strided(o, (*front, H, dv), "out", dtype, dev)
+        desc, at, need = _decay_desc(dt, front[0] if len(front) == 2 else 1, B, H, KV, dk, dv, scale, q0, q1, k0, k1, v0, v1, o0, o1)
+        ws = _op_workspace(need, dev)
+        whole = (B, H, dk, dv)
+        _op_check(lib, lib.seed_op_decay(
+            at, pq, pk, pv, _op_arg(decay, torch.float32, (H,), "decay", dev), _op_arg(done, torch.uint8, front, "done", dev),
+            _op_arg(lengths, torch.int32, (B,), "lengths", dev), _op_arg(state, torch.float32, whole, "state", dev), po,
+            _op_arg(so, torch.float32, whole, "state_out", dev), None if ws is None else ws.data_ptr(), need, handle))
+        return o, so
+
+    return _on_stream(dev, stream, call)
 
 
 def decay_attention(q, k, v, decay, state=None, done=None, lengths=None, scale=1.0, out=None, state_out=None, stream=None):
@@ -566,39 +613,17 @@ def decay_attention(q, k, v, decay, state=None, done=None, lengths=None, scale=1
     uint8; lengths [rows] int32: the steps behind a row's length are neither read nor written (`out` is zero there where
     it is allocated here).  Returns out [steps, rows, heads, value_dim] and the state after the last step; `state_out`
     may be `state` itself."""
-    import torch
-    lib = load_library()
-    dt, dev, dtype = _op_dtype(q, "q"), q.device, q.dtype
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise TypeError("q, k and v must be [steps, rows, heads, dim]")
-    T, B, H, dk = q.shape
-    KV, dv = k.shape[2], v.shape[3]
-    with _OpCall(dev, stream) as call:
-        if out is None:
-            out = (torch.empty if lengths is None else torch.zeros)((T, B, H, dv), dtype=dtype, device=dev)
-        if state_out is None:
-            state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev)
-        pq, q0, q1 = _strided(q, (T, B, H, dk), "q", dtype, dev)
-        pk, k0, k1 = _strided(k, (T, B, KV, dk), "k", dtype, dev)
-        pv, v0, v1 = _strided(v, (T, B, KV, dv), "v", dtype, dev)
-        po, o0, o1 = _strided(out, (T, B, H, dv), "out", dtype, dev)
-        d = SeedDecay(C.sizeof(SeedDecay), dt, T, B, H, KV, dk, dv, scale, q0, q1, k0, k1, v0, v1, o0, o1)
-        ref = C.byref(d)
-        need = lib.seed_op_decay_workspace(ref)
-        ws = call.workspace(need)
-        _op_check(lib, lib.seed_op_decay(
-            ref, pq, pk, pv, _op_arg(decay, torch.float32, (H,), "decay", dev), _op_arg(done, torch.uint8, (T, B), "done", dev),
-            _op_arg(lengths, torch.int32, (B,), "lengths", dev), _op_arg(state, torch.float32, (B, H, dk, dv), "state", dev), po,
-            _op_arg(state_out, torch.float32, (B, H, dk, dv), "state_out", dev), None if ws is None else ws.data_ptr(), need, call.stream))
-    return out, state_out
+    return _decay(q.shape[:2], q, k, v, decay, state, done, lengths, scale, out, state_out, stream)
 
 
 def decay_step(q, k, v, decay, state=None, done=None, scale=1.0, out=None, state_out=None, stream=None):
     """decay_attention for single tokens: q [rows, heads, key_dim], k, v [rows, kv_heads, ...], done [rows], out
     [rows, heads, value_dim]."""
-    out, state_out = decay_attention(q[None], k[None], v[None], decay, state, None if done is None else done[None], None, scale,
-                                     None if out is None else out[None], state_out, stream)
-    return out[0], state_out
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise TypeError("q, k and v must be [rows, heads, dim]")
+    return _decay(q.shape[:1], q, k, v, decay, state, done, None, scale, out, state_out, stream)
 
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", out=None, stream=None):
@@ -606,25 +631,24 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", o
     channels] contiguous, fp32 or bf16; weight and bias [channels] fp32.  `out` may be x itself."""
     import torch
     lib = load_library()
-    dt, dev = _op_dtype(x, "x"), x.device
-    if x.dim() < 2:
+    dt, dev, shape = _op_dtype(x, "x"), x.device, x.shape
+    if len(shape) < 2:
         raise TypeError("x must be [rows, ..., channels]")
     if activation not in _ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
-    N, Cn = x.shape[0], x.shape[-1]
-    P = 1
-    for n in x.shape[1:-1]:
-        P *= n
-    with _OpCall(dev, stream) as call:
-        if out is None:
-            out = torch.empty_like(x)
-        need = lib.seed_op_group_norm_workspace(dt, N, P, Cn, groups)
-        ws = call.workspace(need)
+    N, P, Cn = shape[0], math.prod(shape[1:-1]), shape[-1]
+
+    def call(handle):
+        y = torch.empty_like(x) if out is None else out
+        need = _norm_workspace(dt, N, P, Cn, groups)
+        ws = _op_workspace(need, dev)
         _op_check(lib, lib.seed_op_group_norm(
-            dt, N, P, Cn, groups, _op_arg(x, x.dtype, x.shape, "x", dev), _op_arg(weight, torch.float32, (Cn,), "weight", dev),
-            _op_arg(bias, torch.float32, (Cn,), "bias", dev), eps, _ACTIVATIONS[activation], _op_arg(out, x.dtype, x.shape, "out", dev),
-            None if ws is None else ws.data_ptr(), need, call.stream))
-    return out
+            dt, N, P, Cn, groups, _op_arg(x, x.dtype, shape, "x", dev), _op_arg(weight, torch.float32, (Cn,), "weight", dev),
+            _op_arg(bias, torch.float32, (Cn,), "bias", dev), eps, _ACTIVATIONS[activation], _op_arg(y, x.dtype, shape, "out", dev),
+            None if ws is None else ws.data_ptr(), need, handle))
+        return y
+
+    return _on_stream(dev, stream, call)
 
 
 def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, stream=None):
@@ -638,28 +662,26 @@ def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=Non
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise TypeError("logits must be [rows, choices] with dense rows")
     R, V = logits.shape
-    f32, i32 = torch.float32, torch.int32
-    with _OpCall(dev, stream) as call:
-        if token is None:
-            token = torch.empty(R, dtype=i32, device=dev)
-        if logprob is None:
-            logprob = torch.empty(R, dtype=f32, device=dev)
+    rows, f32, i32 = (R,), torch.float32, torch.int32
 
+    def call(handle):
+        tok = torch.empty(R, dtype=i32, device=dev) if token is None else token
+        lp = torch.empty(R, dtype=f32, device=dev) if logprob is None else logprob
         keep = []
 
         def per_row(x, dtype, name):
-            if x is None:
-                return None
-            if not isinstance(x, torch.Tensor):
-                x = torch.full((R,), x, dtype=dtype, device=dev)
+            if x is not None and not isinstance(x, torch.Tensor):
+                x = torch.full(rows, x, dtype=dtype, device=dev)
                 keep.append(x)
-            return _op_arg(x, dtype, (R,), name, dev)
+            return _op_arg(x, dtype, rows, name, dev)
 
-        need = lib.seed_op_sample_workspace(dt, R, V)
-        ws = call.workspace(need)
+        need = _sample_workspace(dt, R, V)
+        ws = _op_workspace(need, dev)
         _op_check(lib, lib.seed_op_sample(
-            dt, R, V, logits.stride(0), logits.data_ptr(), _op_arg(uniforms, f32, (R,), "uniforms", dev),
+            dt, R, V, logits.stride(0), logits.data_ptr(), _op_arg(uniforms, f32, rows, "uniforms", dev),
             per_row(temperature, f32, "temperature"), per_row(top_k, i32, "top_k"), per_row(top_p, f32, "top_p"), per_row(min_p, f32, "min_p"),
-            _op_arg(token, i32, (R,), "token", dev), _op_arg(logprob, f32, (R,), "logprob", dev),
-            None if ws is None else ws.data_ptr(), need, call.stream))
-    return token, logprob
+            _op_arg(tok, i32, rows, "token", dev), _op_arg(lp, f32, rows, "logprob", dev),
+            None if ws is None else ws.data_ptr(), need, handle))
+        return tok, lp
+
+    return _on_stream(dev, stream, call)
