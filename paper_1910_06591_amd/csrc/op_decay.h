@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
 //
 // Roundings: bf16 inputs are operands as they are.  What is computed between the products is split into bf16 parts whose
 // sum it is: scores and state into two (2^-16 of the value is lost, small beside the output's own 2^-8), the weighted
-// values of the state's update into three (nothing is lost: the state is fp32).  fp32 inputs use the fp32 matrix
+// values of the state's update into three (nothing is lost: the state is fp32) or, where it feeds outputs only, two.  fp32 inputs use the fp32 matrix
 // instructions.
 //
 // A chunk with a value that is not finite is worked on step by step (chunks of one): a product with a zero weight
@@ -631,6 +631,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
 #pragma unroll
         for (int ks = 0; ks < JS; ++ks) {
             constexpr int W = sizeof(T) == 4 ? 1 : 3;
+            // a split time axis has its final state from the segments' own: this one only feeds outputs, two parts do
+            const bool three = !OUT || !split;
             Frag w[W][NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -642,8 +644,10 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                     float x[8] = {bf16_lo_f32(u.x) * wa[0], bf16_hi_f32(u.x) * wa[1], bf16_lo_f32(u.y) * wa[2], bf16_hi_f32(u.y) * wa[3],
                                   bf16_lo_f32(u.z) * wb[0], bf16_hi_f32(u.z) * wb[1], bf16_lo_f32(u.w) * wb[2], bf16_hi_f32(u.w) * wb[3]};
                     w[0][n] = decay_split8(x);
-                    w[1][n] = decay_split8(x);
-                    w[2][n] = decay_round8(x);
+                    if (three) {
+                        w[1][n] = decay_split8(x);
+                        w[2][n] = decay_round8(x);
+                    } else w[1][n] = decay_round8(x);
                 }
             }
 #pragma unroll
@@ -653,10 +657,11 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                 for (int x = 0; x < 4; ++x) fk[x] = *(const Frag*)(ldskt + decay_operand<CROW>(xc, m + x, ks));
 #pragma unroll
                 for (int y = 0; y < W; ++y)
+                    if (y < 2 || three)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
+                        for (int x = 0; x < 4; ++x)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) S[m + x][n] = M::mma(fk[x], w[y][n], S[m + x][n]);
+                            for (int n = 0; n < NT; ++n) S[m + x][n] = M::mma(fk[x], w[y][n], S[m + x][n]);
             }
         }
         __syncthreads();                                     // everything staged is read

@@ -125,26 +125,38 @@ template <class T> struct SampleMem {
         head = min(V, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
         vecs = (V - head) / VEC;
     }
-    // f(value, index) for every element of tile `tile` (NT * U vectors; the head and the tail are tile 0's), in any order
-    template <int NT, int U, class F> __device__ __forceinline__ void tile(int tile, F f) const
+    // f(value, index) for every element of tiles from .. to (NT * U vectors each; the head and the tail are tile 0's), in
+    // any order.  A tile is on its way while the one before it is worked on.
+    template <int NT, int U, class F> __device__ __forceinline__ void sweep(int from, int to, F f) const
     {
         const u32x4* body = (const u32x4*)(x + head);
-        const int first = tile * NT * U + (int)threadIdx.x;
-        u32x4 v[U];
+        u32x4 v[U], next[U];
+        auto load = [&](int tile, u32x4 (&to)[U]) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (first + u * NT < vecs) v[u] = body[first + u * NT];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (first + u * NT < vecs) {
-                const int i = head + (first + u * NT) * VEC;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const uint32_t w = v[u][sizeof(T) == 4 ? e : e / 2];
-                    if constexpr (sizeof(T) == 4) f(__builtin_bit_cast(float, w), i + e);
-                    else f(e & 1 ? bf16_hi_f32(w) : bf16_lo_f32(w), i + e);
-                }
+            for (int u = 0; u < U; ++u) {
+                const int i = (tile * U + u) * NT + (int)threadIdx.x;
+                if (i < vecs) to[u] = body[i];
             }
-        if (tile == 0) {
+        };
+        load(from, v);
+        for (int t = from; t < to; ++t) {
+            if (t + 1 < to) load(t + 1, next);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = (t * U + u) * NT + (int)threadIdx.x;
+                if (at < vecs) {
+                    const int i = head + at * VEC;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const uint32_t w = v[u][sizeof(T) == 4 ? e : e / 2];
+                        if constexpr (sizeof(T) == 4) f(__builtin_bit_cast(float, w), i + e);
+                        else f(e & 1 ? bf16_hi_f32(w) : bf16_lo_f32(w), i + e);
+                    }
+                }
+                v[u] = next[u];
+            }
+        }
+        if (from == 0) {
             if ((int)threadIdx.x < head) f((float)x[threadIdx.x], (int)threadIdx.x);
             const int i = head + vecs * VEC + (int)threadIdx.x;
             if (i < V) f((float)x[i], i);
@@ -283,7 +295,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     auto larger = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
     auto first_key = [&]() {                                 // the first of the order
         uint64_t best = 0;
-        for (int t = 0; t < tiles; ++t) row.template tile<NT, U>(t, [&](float f, int i) { best = larger(best, sample_key(sample_clean(f), i)); });
+        row.template sweep<NT, U>(0, tiles, [&](float f, int i) { best = larger(best, sample_key(sample_clean(f), i)); });
         return sample_reduce<NT>(best, l.scratch, larger);
     };
     auto largest = [&](float f) { return sample_reduce<NT>(f, (float*)l.scratch, [](float a, float b) { return fmaxf(a, b); }); };
@@ -314,7 +326,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     // Choices below `cut` (a logit, a little too low rather than too high) no longer matter.
     float cut;
     float top = -INFINITY;                                   // the largest logit, as far as it is known (NaN is none: fmaxf)
-    row.template tile<NT, U>(0, [&](float f, int) { top = fmaxf(top, f); });
+    row.template sweep<NT, U>(0, 1, [&](float f, int) { top = fmaxf(top, f); });
     top = largest(top);
     bool inf_row = top == INFINITY;                          // +inf among the logits: those are the choices, all equal
     // (below the place's own logit by more than its roundings)
@@ -358,7 +370,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     // the others is not asked for.  If the list does not hold them, the row is taken as a whole below.
     uint64_t* const cand = (uint64_t*)l.run;
     int cands = 0;
-    bool listed = tiles > 1 && !inf_row && top != -INFINITY && (k ? k <= CAP / 2 : min_p > 0.0f && !all_mass);
+    bool listed = tiles > 1 && !inf_row && top != -INFINITY && (k ? k <= CAP / 4 : min_p > 0.0f && !all_mass);
     if (listed) {
         bins.centre = (double)top;
         cut = -FLT_MAX;
@@ -368,14 +380,16 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         };
         if (k) {
             clear();
-            row.template tile<NT, U>(0, [&](float f, int) { const int bin = bin_at(bins.place(f)); if (bin >= 0) atomicAdd(&l.count[bin], 1u); });
+            row.template sweep<NT, U>(0, 1, [&](float f, int) { const int bin = bin_at(bins.place(f)); if (bin >= 0) atomicAdd(&l.count[bin], 1u); });
         }
         narrow();
         __syncthreads();
         if (tid == 0) l.n = 0;
         __syncthreads();
-        for (int t = 0; t < tiles; ++t) {
-            row.template tile<NT, U>(t, [&](float f, int i) {
+        // Behind t tiles another t add about k: there the cut is looked at again, the list then holds some 2 k.
+        for (int t = 0, end; t < tiles; t = end) {
+            end = min(tiles, max(t + 1, t * 2));
+            row.template sweep<NT, U>(t, end, [&](float f, int i) {
                 if (f >= cut) {
                     const int at = atomicAdd(&l.n, 1);
                     if (at < CAP) cand[at] = sample_key(f + 0.0f, i);
@@ -384,7 +398,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
             __syncthreads();
             cands = l.n;
             if (cands > CAP) break;
-            if (cands > CAP / 2 || t == tiles - 1) {         // the centre at the largest so far, the cut anew, and out with what is below it
+            if (cands > 3 * CAP / 8 || end == tiles) {         // the centre at the largest so far, the cut anew, and out with what is below it
                 uint64_t mine[CAP / NT];
                 top = -INFINITY;
 #pragma unroll
@@ -429,8 +443,8 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         cut = min_p > 0.0f && !all_mass && !(k && top_p < 1.0f) ? logit_at(257.0 - 16.0 * log((double)min_p)) : -INFINITY;
         clear();
         float seen = -INFINITY;
-        for (int t = 0; t < tiles; ++t) {
-            row.template tile<NT, U>(t, [&](float f, int i) {
+        for (int t = 0; t < tiles; t = t ? tiles : 1) {
+            row.template sweep<NT, U>(t, t ? tiles : 1, [&](float f, int i) {
                 seen = fmaxf(seen, f);
                 if (!(f >= cut)) return;                     // (NaN neither)
                 if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
@@ -514,11 +528,10 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     if (listed)
         for (int i = tid; i < cands; i += NT) collect(value(cand[i]), (int)~(uint32_t)cand[i]);
     else
-        for (int t = 0; t < tiles; ++t)
-            row.template tile<NT, U>(t, [&](float f, int i) {
-                if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
-                if (f >= cut) collect(f, i);
-            });
+        row.template sweep<NT, U>(0, tiles, [&](float f, int i) {
+            if (inf_row) f = f == INFINITY ? 0.0f : -INFINITY;
+            if (f >= cut) collect(f, i);
+        });
     __syncthreads();
     const int n = l.n;
     if (n > CAP) {                                           // (uniform)
