@@ -7,8 +7,7 @@
 // the mean, squared), never a difference of sums.  Kernels, by shape (norm_launch):
 //   segment   points == 1: a group is a run of channels; a few lanes own it, sums are shuffles.
 //   resident  a row (or a slice of its groups) fits a workgroup's registers: read once, written once.
-//   split     larger rows: statistics of tiles (each held in registers), then a second kernel that joins them and
-//             reads x again.
+//   split     larger rows: statistics of runs of points, then a second kernel that joins them and reads x again.
 //   plain     what is left (more channels than a workgroup has vectors, points > 1).
 #pragma once
 #include <algorithm>
@@ -142,28 +141,23 @@ __global__ __launch_bounds__(256) void norm_plain_kernel(NormArgs p)
         }
 }
 
-// points == 1: L lanes own a group of cg = up to L * E * VEC channels, E vectors a lane, and do K such groups that lie
-// `stride` groups apart, a whole number of rows: their channels, and so weight and bias, are the same.  All loads go out
-// first; with one group a thread a wavefront was over before its loads had paid for its launch (33.5 MB in bf16, 65536
-// groups of 128: 11.6 us, four groups a thread NORM_K4 us).
-template <class T, int VEC, int E, int K>
-__global__ __launch_bounds__(256) void norm_segment_kernel(NormArgs p, int log_lanes, uint32_t segments, uint32_t stride)
+// points == 1: L lanes own a group of cg = up to L * E * VEC channels, E vectors a lane.
+constexpr int NORM_SEGMENT_THREADS = 256;
+template <class T, int VEC, int E>
+__global__ __launch_bounds__(NORM_SEGMENT_THREADS) void norm_segment_kernel(NormArgs p, int log_lanes, uint32_t segments)
 {
     const int L = 1 << log_lanes, cg = p.C / p.G, sub = threadIdx.x & (L - 1);
-    const uint32_t seg0 = (blockIdx.x << (8 - log_lanes)) + (threadIdx.x >> log_lanes);
-    const int ch0 = (int)(seg0 % (uint32_t)p.G) * cg;
-    Pack<T, VEC> d[K][E];
+    const uint32_t seg = blockIdx.x * (NORM_SEGMENT_THREADS >> log_lanes) + (threadIdx.x >> log_lanes);
+    if (seg >= segments) return;                             // (all lanes of a group together)
+    const int ch0 = (int)(seg % (uint32_t)p.G) * cg;
+    const T* x = (const T*)p.x + (size_t)seg * cg;
+    Pack<T, VEC> d[E];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t seg = seg0 + k * stride;              // (below 2^25)
-        const T* x = (const T*)p.x + (size_t)seg * cg;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = (sub + i * L) * VEC;
-            if (seg < segments && c < cg) d[k][i] = *(const Pack<T, VEC>*)(x + c);
-        }
+    for (int i = 0; i < E; ++i) {
+        const int c = (sub + i * L) * VEC;
+        if (c < cg) d[i] = *(const Pack<T, VEC>*)(x + c);
     }
-    float w[E][VEC], b[E][VEC];
+    float w[E][VEC], b[E][VEC], s = 0.0f, m2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         const int c = (sub + i * L) * VEC;
@@ -174,34 +168,28 @@ __global__ __launch_bounds__(256) void norm_segment_kernel(NormArgs p, int log_l
     }
     const float inv = 1.0f / (float)cg;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t seg = seg0 + k * stride;
-        float s = 0.0f;
+    for (int i = 0; i < E; ++i)
+        if ((sub + i * L) * VEC < cg)
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            if ((sub + i * L) * VEC < cg)
+            for (int e = 0; e < VEC; ++e) s += d[i].get(e);
+    for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+    const float mean = s * inv;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s += d[k][i].get(e);
-        for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
-        const float mean = s * inv;
-        float m2 = 0.0f;
+    for (int i = 0; i < E; ++i)
+        if ((sub + i * L) * VEC < cg)
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            if ((sub + i * L) * VEC < cg)
+            for (int e = 0; e < VEC; ++e) { const float f = d[i].get(e) - mean; m2 = fmaf(f, f, m2); }
+    for (int off = L / 2; off > 0; off >>= 1) m2 += __shfl_xor(m2, off, 64);
+    const float rstd = 1.0f / sqrtf(m2 * inv + p.eps);
+    T* y = (T*)p.y + (size_t)seg * cg;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) { const float f = d[k][i].get(e) - mean; m2 = fmaf(f, f, m2); }
-        for (int off = L / 2; off > 0; off >>= 1) m2 += __shfl_xor(m2, off, 64);
-        const float rstd = 1.0f / sqrtf(m2 * inv + p.eps);
-        T* y = (T*)p.y + (size_t)seg * cg;
+    for (int i = 0; i < E; ++i) {
+        const int c = (sub + i * L) * VEC;
+        if (c < cg) {
+            float f[VEC];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = (sub + i * L) * VEC;
-            if (seg < segments && c < cg) {
-                float f[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = norm_finish(d[k][i].get(e) - mean, rstd * w[i][e], b[i][e], p.act);
-                *(Pack<T, VEC>*)(y + c) = norm_pack<T, VEC>(f);
-            }
+            for (int e = 0; e < VEC; ++e) f[e] = norm_finish(d[i].get(e) - mean, rstd * w[i][e], b[i][e], p.act);
+            *(Pack<T, VEC>*)(y + c) = norm_pack<T, VEC>(f);
         }
     }
 }
@@ -388,42 +376,66 @@ __device__ __forceinline__ void norm_join(float& n, float& mean, float& m2, floa
     }
 }
 
-// Split, first kernel: a workgroup per row, slice and run of points, tile by tile; stats[row][group][run] = (mean, sum
-// of squared differences) of the run.
-constexpr int NORM_SPLIT_THREADS = 512, NORM_SPLIT_E = 8, NORM_APPLY_THREADS = 512;
+// Split, first kernel: a workgroup per row, slice and run of points; stats[row][group][run] = (mean, sum of squared
+// differences) of the run.  A thread joins its channels' values batch by batch, each batch held in registers for its two
+// passes, the next one on its way; the threads meet once, at the run's end: with two sums over the workgroup for every
+// batch, their barriers left the memory idle (83 MB read, as many written back: 37 us so, 31 us now, the same for 4 or 8 points
+// a batch and 512 or 1024 workgroups).
+constexpr int NORM_SPLIT_THREADS = 512, NORM_SPLIT_U = 4, NORM_APPLY_THREADS = 1024;
 template <class T, int VEC>
 __global__ __launch_bounds__(NORM_SPLIT_THREADS) void norm_stats_kernel(NormArgs p, int cw, int runs, int run_points, float2* stats)
 {
-    constexpr int NT = NORM_SPLIT_THREADS, E = NORM_SPLIT_E;
+    constexpr int NT = NORM_SPLIT_THREADS, U = NORM_SPLIT_U;
     extern __shared__ float norm_lds[];
     const int cg = p.C / p.G, slices = p.C / cw;
     const NormTile t(cw, cg, VEC, NT);
     float* part = norm_lds;
     float* mean = part + VEC * NT;
     float* m2 = mean + t.groups;
-    float* run_mean = m2 + t.groups;
-    float* run_m2 = run_mean + t.groups;
     const int slice = (int)(blockIdx.x % slices), run = (int)(blockIdx.x / slices % runs);
     const size_t n = blockIdx.x / slices / runs;
-    const int first = run * run_points, last = min(p.P, first + run_points), tile = t.rows * E;
+    const int first = run * run_points, last = min(p.P, first + run_points), tile = t.rows * U;
     const T* x = (const T*)p.x + n * (size_t)p.P * p.C + slice * cw;
-    Pack<T, VEC> d[E], next[E];
-    norm_tile_load<T, VEC, E>(t, x + (size_t)first * p.C, p.C, min(tile, last - first), d);
+    Pack<T, VEC> d[U], next[U];
+    float mu[VEC], sq[VEC], have = 0.0f;                     // of this thread's channels, over `have` points
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) mu[e] = sq[e] = 0.0f;
+    norm_tile_load<T, VEC, U>(t, x + (size_t)first * p.C, p.C, last - first, d);
     for (int at = first; at < last; at += tile) {
-        const int points = min(tile, last - at);
-        // the next tile is on its way while this one is added up
-        if (at + tile < last) norm_tile_load<T, VEC, E>(t, x + (size_t)(at + tile) * p.C, p.C, min(tile, last - at - tile), next);
-        norm_tile_stats<T, VEC, NT, E>(t, points, d, part, mean, m2);
-        for (int g = threadIdx.x; g < t.groups; g += NT) {
-            float cnt = (float)(at - first) * (float)cg, a = at == first ? 0.0f : run_mean[g], b = at == first ? 0.0f : run_m2[g];
-            norm_join(cnt, a, b, (float)points * (float)cg, mean[g], m2[g]);
-            run_mean[g] = a; run_m2[g] = b;                  // (always the same thread's)
+        if (at + tile < last) norm_tile_load<T, VEC, U>(t, x + (size_t)(at + tile) * p.C, p.C, last - at - tile, next);
+        const int left = t.on ? last - at - t.row : 0;       // (u * rows < left: there is a point)
+        if (left > 0) {
+            const float batch = (float)min(U, (left + t.rows - 1) / t.rows), total = have + batch, f = batch / total, inv = 1.0f / batch;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float s = 0.0f, q = 0.0f;
+#pragma unroll
+                for (int u = 0; u < U; ++u) s += u * t.rows < left ? d[u].get(e) : 0.0f;
+                s *= inv;
+#pragma unroll
+                for (int u = 0; u < U; ++u) { const float g = u * t.rows < left ? d[u].get(e) - s : 0.0f; q = fmaf(g, g, q); }
+                const float g = s - mu[e];
+                mu[e] = fmaf(g, f, mu[e]);
+                sq[e] += fmaf(g * g, have * f, q);
+            }
+            have = total;
         }
 #pragma unroll
-        for (int i = 0; i < E; ++i) d[i] = next[i];
+        for (int u = 0; u < U; ++u) d[u] = next[u];
     }
+    float s[VEC], of[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[e] = mu[e] * have;
+    norm_group_sums<VEC, NT>(t, s, part, mean);
+    const float inv = 1.0f / ((float)(last - first) * (float)cg);
+    for (int g = threadIdx.x; g < t.groups; g += NT) mean[g] *= inv;
+    __syncthreads();
+    norm_of_groups<VEC>(mean, t.on ? t.col * VEC : 0, cg, of);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { const float g = mu[e] - of[e]; s[e] = have > 0.0f ? fmaf(g * g, have, sq[e]) : 0.0f; }
+    norm_group_sums<VEC, NT>(t, s, part, m2);
     for (int g = threadIdx.x; g < t.groups; g += NT)
-        stats[(n * p.G + slice * t.groups + g) * runs + run] = make_float2(run_mean[g], run_m2[g]);
+        stats[(n * p.G + slice * t.groups + g) * runs + run] = make_float2(mean[g], m2[g]);
 }
 
 // Split, second kernel: every workgroup joins the runs of its row (a wavefront per group, lanes over runs, always in the
@@ -466,7 +478,7 @@ __global__ __launch_bounds__(NORM_APPLY_THREADS) void norm_apply_kernel(NormArgs
     const size_t base = n * (size_t)p.P * p.C + c0, step = (size_t)t.rows * p.C;
     const uint32_t off = t.offset<VEC>(p.C, sizeof(T));
     const int last = min(p.P, (piece + 1) * part_points);
-    constexpr int U = 4;                                     // loads in flight
+    constexpr int U = 2;                                     // loads in flight
     for (int first = piece * part_points; first < last; first += U * t.rows) {
         const int at = first + t.row;
         const T* x = (const T*)p.x + base + (size_t)first * p.C;
@@ -491,7 +503,7 @@ enum NormKind { NORM_SEGMENT, NORM_RESIDENT, NORM_SPLIT, NORM_PLAIN };
 struct NormPlan {
     NormKind kind;
     int vec;                     // elements a vector
-    int lanes, per_lane, per_thread;               // segment: lanes a group, vectors a lane, groups a thread
+    int lanes, per_lane;         // segment: lanes a group, vectors a lane
     int cw, threads;             // resident, split: channels a slice; resident: threads
     int runs, run_points, parts, part_points;      // split
     size_t workspace;
@@ -511,11 +523,9 @@ static inline NormPlan norm_plan(int N, int P, int C, int G, int size, int vec)
         while (cg % v) v /= 2;
         const int n = cg / v;
         int lanes = 1;
-        while (lanes < n && lanes < 64) lanes *= 2;
+        while (lanes * 2 < n && lanes < 64) lanes *= 2;          // (two vectors a lane: 33.5 MB in 65536 groups of 128, bf16: 9.4 us; one: 10.1, four: 10.7)
         if (n <= lanes * 8) {
             q.kind = NORM_SEGMENT; q.vec = v; q.lanes = lanes; q.per_lane = (n + lanes - 1) / lanes;
-            // four groups a thread where that still leaves every compute unit two wavefronts on each SIMD
-            q.per_thread = q.per_lane <= 2 && (int64_t)N * G * lanes >= (int64_t)4 * 256 * 512 ? 4 : 1;
             return q;
         }
     }
@@ -526,27 +536,29 @@ static inline NormPlan norm_plan(int N, int P, int C, int G, int size, int vec)
     int best = 0, widest = 0;
     for (int k = 1; k <= C / unit && !(wide && P > 1); ++k) {
         const int cw = unit * k;
-        if (C % cw || cw / vec > 1024 || cw / cg > 2048) continue;
+        if (cw / vec > 1024 || cw / cg > 2048) break;
+        if (C % cw) continue;
         if (cw * size < 128 && cw != C) continue;
         if (cw / vec <= 256) widest = cw;
         // the widest slice that fits, but narrower ones while the rows alone leave compute units without work
         if (fits(cw, 1024, 8) && (!best || (int64_t)N * (C / cw) >= 256)) best = cw;
     }
-    if (best) {
+    if (best && C / best <= 1 << 20) {                       // (a row's workgroups fit a launch)
         q.kind = NORM_RESIDENT; q.cw = best;
         q.threads = fits(best, 256, 4) ? 256 : fits(best, 512, 8) ? 512 : 1024;
         return q;
     }
     if (!widest || P == 1) { q.kind = NORM_PLAIN; return q; }
     q.kind = NORM_SPLIT; q.cw = widest;
-    // runs of whole tiles, about 512 workgroups (two a compute unit), at most 256 a row (every workgroup of the second
+    // about 512 workgroups (two a compute unit) of at least a batch, at most 256 a row (every workgroup of the second
     // kernel reads them all)
-    const int tile = NORM_SPLIT_THREADS / (widest / vec) * NORM_SPLIT_E, tiles = (P + tile - 1) / tile;
+    const int tile = NORM_SPLIT_THREADS / (widest / vec) * NORM_SPLIT_U;
     const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(1, (int64_t)N * (C / widest)));
-    const int runs = (int)std::min<int64_t>(std::min<int64_t>(want, 256), tiles);
-    q.run_points = (tiles + runs - 1) / runs * tile;
+    const int64_t runs = std::min<int64_t>(std::min<int64_t>(want, 256), (P + tile - 1) / tile);
+    q.run_points = (int)((P + runs - 1) / runs);
     q.runs = (P + q.run_points - 1) / q.run_points;
-    const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(1, (int64_t)N * (C / widest)), (P + 31) / 32));
+    // second kernel: 512 workgroups of 1024 threads (83 MB read and written: 34 us; 1024 of 512 threads: 40 us)
+    const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(1, (int64_t)N * (C / widest)), (P + 31) / 32));
     q.part_points = (int)((P + pieces - 1) / pieces);
     q.parts = (P + q.part_points - 1) / q.part_points;
     q.workspace = (size_t)N * q.runs * G * sizeof(float2);
@@ -558,39 +570,46 @@ static void norm_launch_vec(const NormArgs& p, const NormPlan& q, void* workspac
 {
     const int cg = p.C / p.G;
     if (q.kind == NORM_SEGMENT) {
-        const uint32_t segments = (uint32_t)((size_t)p.N * p.G), per = 256 / q.lanes;       // (at most 2^23)
-        // whole rows between a thread's groups: per * blocks is a multiple of G
-        const uint32_t k = q.per_thread, some = (uint32_t)p.G / std::gcd((uint32_t)p.G, per);
-        uint32_t blocks = (segments + per * k - 1) / (per * k);
-        if (k > 1) blocks = (blocks + some - 1) / some * some;
+        const uint32_t segments = (uint32_t)((size_t)p.N * p.G), per = NORM_SEGMENT_THREADS / q.lanes;
         const int log_lanes = __builtin_ctz(q.lanes);
-        auto go = [&](auto e, auto kk) {
-            hipLaunchKernelGGL((norm_segment_kernel<T, VEC, decltype(e)::value, decltype(kk)::value>), dim3(blocks), dim3(256), 0, s, p, log_lanes, segments, per * blocks);
+        auto go = [&](auto e) {
+            hipLaunchKernelGGL((norm_segment_kernel<T, VEC, decltype(e)::value>), dim3((segments + per - 1) / per), dim3(NORM_SEGMENT_THREADS), 0, s, p, log_lanes, segments);
         };
         using I1 = std::integral_constant<int, 1>; using I2 = std::integral_constant<int, 2>; using I4 = std::integral_constant<int, 4>; using I8 = std::integral_constant<int, 8>;
-        if (q.per_lane == 1) { if (k == 4) go(I1{}, I4{}); else go(I1{}, I1{}); }
-        else if (q.per_lane == 2) { if (k == 4) go(I2{}, I4{}); else go(I2{}, I1{}); }
-        else if (q.per_lane <= 4) go(I4{}, I1{});
-        else go(I8{}, I1{});
-    } else if (q.kind == NORM_RESIDENT) {
-        const dim3 grid((unsigned)((size_t)p.N * (p.C / q.cw)));
-        const size_t lds = (size_t)(VEC * q.threads + 2 * (q.cw / cg)) * sizeof(float);
-        const int rows = q.threads / (q.cw / VEC), e = (p.P + rows - 1) / rows;
-        auto go = [&](auto nt, auto ee) {
-            constexpr int NT = decltype(nt)::value, E = decltype(ee)::value;
-            hipLaunchKernelGGL((norm_resident_kernel<T, VEC, NT, E>), grid, dim3(NT), lds, s, p, q.cw);
-        };
-        using I2 = std::integral_constant<int, 2>; using I4 = std::integral_constant<int, 4>; using I8 = std::integral_constant<int, 8>;
-        if (q.threads == 256) { if (e <= 2) go(std::integral_constant<int, 256>{}, I2{}); else go(std::integral_constant<int, 256>{}, I4{}); }
-        else if (q.threads == 512) go(std::integral_constant<int, 512>{}, I8{});
-        else if (e <= 7) go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 7>{});
-        else go(std::integral_constant<int, 1024>{}, I8{});
-    } else {
-        const int slices = p.C / q.cw, groups = q.cw / cg;
-        hipLaunchKernelGGL((norm_stats_kernel<T, VEC>), dim3((unsigned)((size_t)p.N * q.runs * slices)), dim3(NORM_SPLIT_THREADS),
-                           (size_t)(VEC * NORM_SPLIT_THREADS + 4 * groups) * sizeof(float), s, p, q.cw, q.runs, q.run_points, (float2*)workspace);
-        hipLaunchKernelGGL((norm_apply_kernel<T, VEC>), dim3((unsigned)((size_t)p.N * q.parts * slices)), dim3(NORM_APPLY_THREADS), (size_t)2 * groups * sizeof(float), s,
-                           p, q.cw, q.runs, q.run_points, (const float2*)workspace, q.parts, q.part_points);
+        if (q.per_lane == 1) go(I1{});
+        else if (q.per_lane == 2) go(I2{});
+        else if (q.per_lane <= 4) go(I4{});
+        else go(I8{});
+        return;
+    }
+    // at most 2^21 workgroups a launch (a grid's threads stay below 2^32); runs and parts are more than one only where
+    // rows and slices are few.  (slices are at most 2^20: norm_plan, and 2^20 / 128 where points > 1)
+    const int slices = p.C / q.cw, groups = q.cw / cg, most = (1 << 21) / slices;
+    for (int first = 0; first < p.N; first += most) {
+        NormArgs a = p;
+        a.N = std::min(most, p.N - first);
+        a.x = (const T*)p.x + (size_t)first * p.P * p.C;
+        a.y = (T*)p.y + (size_t)first * p.P * p.C;
+        const unsigned blocks = (unsigned)a.N * slices;
+        if (q.kind == NORM_RESIDENT) {
+            const size_t lds = (size_t)(VEC * q.threads + 2 * groups) * sizeof(float);
+            const int rows = q.threads / (q.cw / VEC), e = (p.P + rows - 1) / rows;
+            auto go = [&](auto nt, auto ee) {
+                constexpr int NT = decltype(nt)::value, E = decltype(ee)::value;
+                hipLaunchKernelGGL((norm_resident_kernel<T, VEC, NT, E>), dim3(blocks), dim3(NT), lds, s, a, q.cw);
+            };
+            using I2 = std::integral_constant<int, 2>; using I4 = std::integral_constant<int, 4>; using I8 = std::integral_constant<int, 8>;
+            if (q.threads == 256) { if (e <= 2) go(std::integral_constant<int, 256>{}, I2{}); else go(std::integral_constant<int, 256>{}, I4{}); }
+            else if (q.threads == 512) go(std::integral_constant<int, 512>{}, I8{});
+            else if (e <= 7) go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 7>{});
+            else go(std::integral_constant<int, 1024>{}, I8{});
+        } else {
+            float2* stats = (float2*)workspace + (size_t)first * q.runs * p.G;
+            hipLaunchKernelGGL((norm_stats_kernel<T, VEC>), dim3(blocks * q.runs), dim3(NORM_SPLIT_THREADS),
+                               (size_t)(VEC * NORM_SPLIT_THREADS + 2 * groups) * sizeof(float), s, a, q.cw, q.runs, q.run_points, stats);
+            hipLaunchKernelGGL((norm_apply_kernel<T, VEC>), dim3(blocks * q.parts), dim3(NORM_APPLY_THREADS), (size_t)2 * groups * sizeof(float), s,
+                               a, q.cw, q.runs, q.run_points, (const float2*)stats, q.parts, q.part_points);
+        }
     }
 }
 

@@ -145,3 +145,15 @@ def test_nothing_to_do_and_refusals():
         seedinf.group_norm(x, 2, activation="tanh")
     with pytest.raises(seedinf.SeedError):
         seedinf.group_norm(x, 3)
+
+
+def test_more_workgroups_than_one_launch_takes():
+    """2^21 + 3 rows of 1025 points of one channel, bf16: offsets past 2^32 bytes, and a grid of more than 2^21 workgroups of 512 threads."""
+    import torch
+    N, P = (1 << 21) + 3, 1025
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB")
+    x = torch.empty(N, P, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(3))
+    y = seedinf.group_norm(x, 1, activation="relu")
+    for rows in (slice(0, 5), slice((1 << 21) - 4, N)):
+        check(x[rows], y[rows], 1, None, None, "relu")
