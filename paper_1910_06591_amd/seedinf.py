@@ -11,6 +11,7 @@ import functools
 import math
 import os
 import subprocess
+import tempfile
 
 import numpy as np
 
@@ -79,14 +80,21 @@ class SeedArch(C.Structure):
 
 def build_library(verbose: bool = False) -> str:
     """Compile csrc/ into libseedinf.so (and the measurement probes into
-    libseedprobe.so) for gfx950 with hipcc (cross-compiles without a GPU)."""
-    for srcs, out in (((SOURCES[0], OP_SOURCES[0]), LIB_PATH), ((PROBE_SOURCE,), PROBE_LIB_PATH)):
-        cmd = ["hipcc", *HIPCC_FLAGS, *srcs, "-o", out]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + r.stderr)
-        if verbose:
-            print(" ".join(cmd))
+    libseedprobe.so) for gfx950 with hipcc (cross-compiles without a GPU), the sources side by side."""
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in (SOURCES[0], OP_SOURCES[0])]
+        stages = [[["hipcc", *flags, "-c", s, "-o", o] for s, o in zip((SOURCES[0], OP_SOURCES[0]), objects)]
+                  + [["hipcc", *HIPCC_FLAGS, PROBE_SOURCE, "-o", PROBE_LIB_PATH]],
+                  [["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB_PATH]]]
+        for stage in stages:
+            running = [(cmd, subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)) for cmd in stage]
+            failed = [err for cmd, p in running for err in [p.communicate()[1]] if p.returncode != 0]
+            if failed:
+                raise RuntimeError("hipcc failed:\n" + "\n".join(failed))
+            if verbose:
+                for cmd in stage:
+                    print(" ".join(cmd))
     return LIB_PATH
 
 
