@@ -522,6 +522,12 @@ def _op_arg(t, dtype, shape, name, device):
     return t.data_ptr()
 
 
+def _op_sizes(*sizes):
+    """The C structs' sizes are 32 bits wide, and ctypes would cut a larger one."""
+    if max(sizes) >= 1 << 31:
+        raise TypeError(f"a size is 2^31 or more: {sizes}")
+
+
 @functools.lru_cache(maxsize=1)
 def _raw_calls():
     """(current device, current stream's handle on a device): torch's own calls without the objects it wraps round them,
@@ -590,6 +596,7 @@ def _decay(front, q, k, v, decay, state, done, lengths, scale, out, state_out, s
     lib = load_library()
     dt, dev, dtype = _op_dtype(q, "q"), q.device, q.dtype
     B, (H, dk), KV, dv = front[-1], q.shape[-2:], k.shape[-2], v.shape[-1]
+    _op_sizes(*front, H, KV, dk, dv)
 
     def call(handle):
         o = out
@@ -645,6 +652,7 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", o
     if activation not in _ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
     N, P, Cn = shape[0], math.prod(shape[1:-1]), shape[-1]
+    _op_sizes(N, P, Cn, groups)
 
     def call(handle):
         y = torch.empty_like(x) if out is None else out
@@ -670,6 +678,7 @@ def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=Non
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise TypeError("logits must be [rows, choices] with dense rows")
     R, V = logits.shape
+    _op_sizes(R, V)
     rows, f32, i32 = (R,), torch.float32, torch.int32
 
     def call(handle):

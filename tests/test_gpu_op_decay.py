@@ -67,6 +67,29 @@ def test_episode_flags(T, B, done, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("done", [0.0, 0.002])
+def test_few_states_and_a_long_axis(done, dtype):
+    """The axis in segments: rows that end inside one, at its end and in front of it, with flags and without."""
+    x = make(5003, 3, 2, 1, 64, 128, dtype, seed=41, done=done, lengths=[5003, 2048, 1])
+    out, state = seedinf.decay_attention(**x)
+    check(x, out, state, 1.0, dtype == "bf16")
+
+
+def test_two_calls_at_once():
+    """Long calls on two streams, each with a workspace of its own, give what they give alone."""
+    import torch
+    xs = [make(6000, 2, 4, 4, 128, 128, "bf16", seed=50 + i) for i in range(2)]
+    alone = [seedinf.decay_attention(**x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(3):
+        both = [seedinf.decay_attention(**x, stream=s.cuda_stream) for x, s in zip(xs, streams)]
+        torch.cuda.synchronize()
+        for (o, t), (wo, wt) in zip(both, alone):
+            assert torch.equal(o, wo) and torch.equal(t, wt)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("T", [5, 40, 140, 700])
 def test_lengths(T, dtype):
     """Steps behind a row's length: inputs (NaN here) are not read, outputs stay as they were, the state is the one at the length."""
@@ -149,7 +172,7 @@ def test_state_in_place_and_handed_over(T):
     check(x, torch.cat([oa, ob]), sb, 1.0, True)
 
 
-@pytest.mark.parametrize("T", [9, 90, 600])
+@pytest.mark.parametrize("T", [9, 90, 600, 5000])
 def test_values_that_are_not_finite_stay_in_their_episode(T):
     """An infinite key or a NaN value reaches the later steps of its episode only: not the steps before it, not the
     episode behind the next flag, not the state after that, and no other row or head."""

@@ -196,3 +196,35 @@ def test_refusals_and_nothing_to_do():
             seedinf.sample(**dict(dict(logits=x, uniforms=u), **bad))
     with pytest.raises(seedinf.SeedError):
         seedinf.sample(torch.zeros(4, 0, device="cuda"), u)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("k,p,m", [(None, None, None), (50, None, None), (None, 0.9, None), (None, None, 0.02), (1000, 0.95, 0.001),
+                                   (1024, 0.5, None), (1025, 0.99, None), (30000, 0.9, 0.01), (3, 0.0, 1.0)])
+def test_long_rows_that_are_not_what_their_beginning_says(k, p, m, dtype):
+    """Rising and falling rows, a beginning that is masked, a last choice far above the others, rows that are all but flat,
+    masks in most places, temperatures that gather all mass in one choice or spread it over all."""
+    import torch
+    V = 70001
+    rng = np.random.default_rng(9)
+    line, noise = np.linspace(-12, 12, V), rng.standard_normal(V)
+    rows = [line, -line, noise, noise.copy(), noise.copy(), 1e-3 * noise, np.where(rng.random(V) < 0.999, -np.inf, noise), 300 * noise, 1e-38 * noise]
+    rows[3][:40000] = -np.inf
+    rows[4][-1] = 500.0
+    x = torch.from_numpy(np.repeat(np.stack(rows), 4, 0).astype(np.float32)).cuda().to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+    R = x.shape[0]
+    a = dict(logits=x, uniforms=rng.random(R, dtype=np.float32), temperature=np.resize(np.float32([1.0, 0.05, 8.0, 1e-38]), R))
+    a.update({n: np.resize(f(v), R) for n, v, f in (("top_k", k, np.int32), ("top_p", p, np.float32), ("min_p", m, np.float32)) if v is not None})
+    check(a)
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Sizes that a 32-bit field would wrap."""
+    import torch
+    one = torch.zeros(1, 4, device="cuda")
+    with pytest.raises((TypeError, seedinf.SeedError)):
+        seedinf.sample(one.expand((1 << 32) + 1, 4), torch.zeros(1, device="cuda"))
+    with pytest.raises((TypeError, seedinf.SeedError)):
+        seedinf.group_norm(one.expand((1 << 32) + 1, 4), 2)
+    with pytest.raises((TypeError, seedinf.SeedError)):
+        seedinf.decay_step(*(one[None].expand((1 << 32) + 1, 1, 4) for _ in range(3)), torch.ones(1, device="cuda"))
