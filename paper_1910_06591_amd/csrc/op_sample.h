@@ -7,10 +7,12 @@
 //   lanes  up to 64: a choice a lane, ranks by counting.
 //   row    a workgroup a row: one pass over the row adds every choice's mass to a histogram over the logit (2048 bins of
 //          1/16 of a temperature); what the filters and the draw ask for is then known up to a few bins; a second pass
-//          collects those bins' choices, which are sorted and searched.  A row that top-k or min-p leaves few choices
+//          collects those bins' choices, which are sorted and searched.  What bounds it: the operations in 64 bits and the LDS additions of the first pass, then some
+//          twenty dependent phases of 1 - 3 us, with few rows on as few compute units.  A row that top-k or min-p leaves few choices
 //          is read once: those go into a list that takes the row's place.
 //          Where the bins hold more choices than fit (logits that are all but equal), the questions are answered one
-//          by one instead, by radix searches over the row (sample_find).
+//          by one instead, by radix searches over the row (sample_find; 64 x 50001 within a hundredth of a temperature:
+//          190 us, with top-p 290, where spread logits take 40).
 #pragma once
 #include <atomic>
 #include <cfloat>
@@ -99,6 +101,20 @@ __device__ __forceinline__ void sample_scan(V* a, int n, V* scratch)
         if (at < n) a[at] = waves + before + x[i];
     }
     __syncthreads();
+}
+
+// The first place of [from, to) that cond, which holds for all behind one that it holds for, holds for; `none` if there
+// is none.  At most 4096 places: the 64 lanes look at the ends of as many parts, then at one part.  Every wavefront
+// for itself, without barriers.
+template <class F> __device__ __forceinline__ int sample_first_of(int from, int to, int none, F cond)
+{
+    const int n = to - from, part = (n + 63) / 64, lane = threadIdx.x & 63;
+    if (n <= 0) return none;
+    uint64_t some = __ballot(cond(from + min(lane * part + part, n) - 1));
+    if (!some) return none;
+    from += (int)__builtin_ctzll(some) * part;
+    some = __ballot(cond(min(from + lane, to - 1)));
+    return some ? min(from + (int)__builtin_ctzll(some), to - 1) : from + part - 1;      // (there is one, but for a sum's last bit)
 }
 
 // ---- a row of memory: 16-byte vectors between a head and a tail of single elements ----
@@ -205,78 +221,85 @@ struct SampleRow {
     __device__ __forceinline__ uint64_t units(double m) const { return (uint64_t)(m * unit + 0.5); }
 };
 
-// One place of the order, from the largest key down, 11 bits of the key a pass: the first element at which the running
-// count reaches `count` (mass = false), or the running mass reaches (strict = false) or exceeds (strict = true) `limit`.
-// Returns its key.  There has to be one.
+// One place of the order: the first element at which the running count reaches `count` (mass = false), or the running mass
+// reaches (strict = false) or exceeds (strict = true) `limit`.  Returns its key.  There has to be one.
+// Digits of the key from the top, up to 11 bits a pass over the row: three for the logit, those that V needs for the index.
+// A thread adds its choices up while they have the same digit (in rows of equal logits all have).
 template <class T, int NT>
-__device__ __forceinline__ uint64_t sample_find(const T* x, int V, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
-                                                          uint64_t* hist, uint64_t* share)
+__device__ __forceinline__ uint64_t sample_find(const SampleMem<T>& x, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
+                                                uint64_t* hist, uint64_t* scratch)
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, index_bits = 32 - __builtin_clz(max(x.V - 1, 1));
     uint64_t prefix = 0, before = 0;
     int low = 64;                                            // key bits below `low` are not yet known
     while (low > 0) {
-        const int w = low < SAMPLE_BITS ? low : SAMPLE_BITS, at = low - w;
+        if (low == 32 && index_bits < 32) {                  // (the index is inverted: ones above its bits)
+            prefix = prefix << (32 - index_bits) | ((1ull << (32 - index_bits)) - 1);
+            low = index_bits;
+        }
+        const int w = low > 32 ? min(SAMPLE_BITS, low - 32) : min(SAMPLE_BITS, low), at = low - w, bins = 1 << w;
+        __syncthreads();                                     // (the previous pass's readers are done)
         for (int i = tid; i < SAMPLE_BINS; i += NT) hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < V; i += NT) {
-            const float f = sample_clean((float)x[i]);
+        int digit = 0;
+        uint64_t sum = 0;
+        x.template sweep<NT, 2>(0, x.template tiles<NT, 2>(), [&](float f, int i) {
+            f = sample_clean(f);
             const uint64_t key = sample_key(f, i);
-            if (low < 64 && (key >> low) != prefix) continue;
-            const uint64_t add = mass ? row.units(row.mass(f)) : 1;
-            if (add) atomicAdd((unsigned long long*)&hist[(key >> at) & ((1u << w) - 1)], (unsigned long long)add);
-        }
-        __syncthreads();
-        if (tid == 0) {                                      // bins from the top
-            uint64_t run = before;
-            int bin = (1 << w) - 1;
-            for (; bin > 0; --bin) {
-                const uint64_t next = run + hist[bin];
-                if (mass ? (strict ? (double)next > limit : (double)next >= limit) && hist[bin] : next >= count) break;
-                run = next;
+            if (low < 64 && (key >> low) != prefix) return;
+            const int d = bins - 1 - (int)((key >> at) & (bins - 1));        // (larger keys first)
+            if (d != digit) {
+                if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
+                digit = d; sum = 0;
             }
-            share[0] = (uint64_t)bin;
-            share[1] = run;
-        }
+            sum += mass ? row.units(row.mass(f)) : 1;
+        });
+        if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
         __syncthreads();
-        prefix = prefix << w | share[0];
-        before = share[1];
+        sample_scan<NT, SAMPLE_BINS / NT>(hist, SAMPLE_BINS, scratch);
+        const int d = sample_first_of(0, bins, bins - 1, [&](int b) {
+            const uint64_t run = before + hist[b];
+            return mass ? (strict ? (double)run > limit : (double)run >= limit) : run >= count;
+        });
+        if (d > 0) before += hist[d - 1];
+        prefix = prefix << w | (uint64_t)(bins - 1 - d);
         low = at;
-        __syncthreads();
     }
+    __syncthreads();
     return prefix;
 }
 
 // The filters and the draw of one row by such searches.  hist: SAMPLE_BINS values; best: the first key of the order.
 template <class T, int NT>
-__device__ __forceinline__ void sample_by_search(const SampleArgs& p, int r, const T* x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
-                                                           uint64_t* hist, uint64_t* scratch, uint64_t* share)
+__device__ __forceinline__ void sample_by_search(const SampleArgs& p, int r, const SampleMem<T>& x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
+                                                 uint64_t* hist, uint64_t* scratch)
 {
     const int tid = threadIdx.x;
     uint64_t last = 0;                                       // the last kept key
-    if (k > 0) last = sample_find<T, NT>(x, p.V, row, false, false, (uint64_t)k, 0.0, hist, share);
-    auto total = [&](double least) {
-        uint64_t s = 0;
-        for (int i = tid; i < p.V; i += NT) {
-            const float f = sample_clean((float)x[i]);
-            const uint64_t key = sample_key(f, i);
-            if (key < last) continue;
-            const double m = row.mass(f);
-            if (m >= least || key == best) s += row.units(m);
+    double z = 0.0;
+    // top-k, top-p, the draw: one after the other, by one piece of code
+    for (int question = k > 0 ? 0 : top_p < 1.0f ? 1 : 2; question < 3; question = question == 0 && top_p < 1.0f ? 1 : question < 2 ? 2 : 3) {
+        double limit = 0.0;
+        if (question > 0) {
+            const double least = question == 2 && min_p > 0.0f ? (double)min_p : 0.0;
+            uint64_t s = 0;
+            x.template sweep<NT, 2>(0, x.template tiles<NT, 2>(), [&](float f, int i) {
+                f = sample_clean(f);
+                const uint64_t key = sample_key(f, i);
+                if (key < last) return;
+                const double m = row.mass(f);
+                if (m >= least || key == best) s += row.units(m);
+            });
+            z = (double)sample_reduce<NT>(s, scratch, [](uint64_t a, uint64_t b) { return a + b; });
+            limit = (question == 1 ? (double)top_p : (double)u) * z;
         }
-        return sample_reduce<NT>(s, scratch, [](uint64_t a, uint64_t b) { return a + b; });
-    };
-    if (top_p < 1.0f) {
-        const double limit = (double)top_p * (double)total(0.0);
-        const uint64_t at = limit > 0.0 ? sample_find<T, NT>(x, p.V, row, true, false, 0, limit, hist, share) : best;
-        last = at > last ? at : last;
-    }
-    const uint64_t z = total(min_p > 0.0f ? (double)min_p : 0.0);
-    const uint64_t at = sample_find<T, NT>(x, p.V, row, true, true, 0, (double)u * (double)z, hist, share);
-    if (tid == 0) {
-        const int i = min((int)(~(uint32_t)at & 0x7fffffffu), p.V - 1);
-        p.token[r] = i;
-        if (p.logprob) p.logprob[r] = (float)(row.exponent(sample_clean((float)x[i])) - log((double)z / row.unit));
+        const uint64_t at = question == 1 && !(limit > 0.0) ? best : sample_find<T, NT>(x, row, question > 0, question == 2, (uint64_t)k, limit, hist, scratch);
+        if (question < 2) last = at > last ? at : last;
+        else if (tid == 0) {
+            const int i = min((int)(~(uint32_t)at & 0x7fffffffu), p.V - 1);
+            p.token[r] = i;
+            if (p.logprob) p.logprob[r] = (float)(row.exponent(sample_clean((float)x.x[i])) - log(z / row.unit));
+        }
     }
 }
 
@@ -321,7 +344,7 @@ template <int CAP> struct SampleLds {
     uint64_t list[CAP];                                      // keys of the collected choices
     double run[CAP];                                         // running sums over them
     uint32_t wanted[SAMPLE_BINS / 32], near[SAMPLE_BINS / 32];       // bits of the bins to collect; of those and their neighbours
-    uint64_t scratch[16], share[2];
+    uint64_t scratch[16];
     int found, n;
 };
 
@@ -520,19 +543,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     __syncthreads();
     sample_scan<NT, NB / NT>(cum, NB, (double*)l.scratch);
     if (k) sample_scan<NT, NB / NT>(l.count, NB, (uint32_t*)l.scratch);
-    // The first place of [from, to) that cond, which holds for all behind one that it holds for, holds for; `none` if there
-    // is none.  At most 4096 places: the 64 lanes look at the ends of as many parts, then at one part.  Every wavefront
-    // for itself, without barriers.
-    auto first_of = [&](int from, int to, int none, auto cond) {
-        const int n = to - from, part = (n + 63) / 64, lane = tid & 63;
-        if (n <= 0) return none;
-        uint64_t some = __ballot(cond(from + min(lane * part + part, n) - 1));
-        if (!some) return none;
-        from += (int)__builtin_ctzll(some) * part;
-        some = __ballot(cond(min(from + lane, to - 1)));
-        return some ? min(from + (int)__builtin_ctzll(some), to - 1) : from + part - 1;      // (there is one, but for a sum's last bit)
-    };
-    auto first_bin = [&](auto cond) { return first_of(0, NB, NB - 1, cond); };
+    auto first_bin = [&](auto cond) { return sample_first_of(0, NB, NB - 1, cond); };
     auto before = [&](int b) { return b > 0 ? cum[b - 1] : 0.0; };
     const double z_all = cum[NB - 1];
     // The last kept choice lies in bin kb (top-k), between pb0 and pb1 (top-p), in mb (min-p); what is drawn between db0 and db1.
@@ -610,7 +621,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         sr.top = top; sr.inv_t = bins.inv_t; sr.unit = (double)(1ull << p.shift);
         __syncthreads();
         const uint64_t best = first_key();
-        sample_by_search<T, NT>(p, r, row.x, sr, best, k, top_p, min_p, u01, l.hist, l.scratch, l.share);
+        sample_by_search<T, NT>(p, r, row, sr, best, k, top_p, min_p, u01, l.hist, l.scratch);
         return;
     }
     // sort them, larger keys first: up to 256 by counting those in front of each, with several threads for one where there are
@@ -670,8 +681,8 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     if (tid >= 64) return;                                   // the rest is one wavefront's
     auto bin_of = [&](int i) { return bins.bin(place_of(l.list[i])); };
     auto range = [&](int b, int& from, int& to) {            // [from, to): the list's part of bin b
-        from = first_of(0, n, n, [&](int i) { return bin_of(i) >= b; });
-        to = first_of(from, n, n, [&](int i) { return bin_of(i) > b; });
+        from = sample_first_of(0, n, n, [&](int i) { return bin_of(i) >= b; });
+        to = sample_first_of(from, n, n, [&](int i) { return bin_of(i) > b; });
     };
     auto sum_at = [&](int i, int from, int b) { return before(b) + (l.run[i] - (from > 0 ? l.run[from - 1] : 0.0)); };
     double z = z_all;                                        // mass of the kept ones
@@ -689,13 +700,13 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
         const double limit = (double)top_p * z;
         const int b = first_bin([&](int b) { return cum[b] >= limit && cum[b] > 0.0; });
         range(b, f, t);
-        const int at = first_of(f, t, t - 1, [&](int i) { return sum_at(i, f, b) >= limit; });
+        const int at = sample_first_of(f, t, t - 1, [&](int i) { return sum_at(i, f, b) >= limit; });
         const double zp = f < t ? sum_at(at, f, b) : cum[b];
         if (b < end || (b == end && zp < z)) { end = b; z = zp; }
     }
     if (mb < NB - 1 && mb <= end) {
         range(mb, f, t);
-        const int at = first_of(f, t, t, [&](int i) { return place_of(l.list[i]) > m_place; }) - 1;      // the last that is kept
+        const int at = sample_first_of(f, t, t, [&](int i) { return place_of(l.list[i]) > m_place; }) - 1;      // the last that is kept
         const double zm = at >= f ? sum_at(at, f, mb) : before(mb);
         if (mb < end || zm < z) { end = mb; z = zm; }
     }
@@ -706,7 +717,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     const double limit = (double)u01 * z;
     const int b = first_bin([&](int b) { return cum[b] > limit; });
     range(b, f, t);
-    const int at = first_of(f, t, max(t - 1, 0), [&](int i) { return sum_at(i, f, b) > limit; });
+    const int at = sample_first_of(f, t, max(t - 1, 0), [&](int i) { return sum_at(i, f, b) > limit; });
     if (tid == 0) {
         const uint64_t key = l.list[at];
         p.token[r] = (int)~(uint32_t)key;
