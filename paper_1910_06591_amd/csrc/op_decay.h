@@ -37,6 +37,8 @@ __device__ __forceinline__ int decay_length(const DecayArgs& p, int b)
 // The recurrence step by step: one workgroup holds dk x 64 of a head's state in registers (a thread 4 columns of
 // every 16th row) and walks the steps.  State columns are independent of one another, so a wider value is several
 // workgroups.  A step's o is a sum over dk: 4 rows of a wavefront by shuffles, the 4 wavefronts through LDS.
+// Bound by the state, read and written once: one step of 256 rows, 16 heads of 128 x 128 (537 MB) 101 us, 5.3 TB/s,
+// what a large copy reaches; 8 rows of 4 heads of 64 x 64 4.2 us, a launch's own time.
 constexpr int DECAY_COLS = 64;
 template <class T, int DK>
 __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
@@ -130,8 +132,15 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
 //
 // Roundings: bf16 inputs are operands as they are.  What is computed between the products is split into bf16 parts whose
 // sum it is: scores and state into two (2^-16 of the value is lost, small beside the output's own 2^-8), the weighted
-// values of the state's update into three (nothing is lost: the state is fp32) or, where it feeds outputs only, two.  fp32 inputs use the fp32 matrix
-// instructions.
+// values of the state's update into three (nothing is lost: the state is fp32) or, where it feeds outputs only, two (long
+// case: 247 us with three, 236 with two).  fp32 inputs use the fp32 matrix instructions.
+//
+// What bounds it: not the bytes (32768 steps of 16 heads of 128 x 128, bf16: 537 MB are 100 us), but a chunk's phases,
+// each of which waits for the one before it: LDS writes of keys and values with their steps side by side, scores, their
+// split, the products with the state in accumulators.  Two workgroups a compute unit fill one another's gaps as far as
+// registers (256 a lane) and LDS (80 KiB) allow.  Split into 32 segments: what they add to the state 87 us, the scan
+// of the states 19, the outputs 135; 4 prompts of up to 4001 steps in 8 segments: 37 + 17 + 64; fp32, 32 steps of 128 rows
+// of 4 heads of 64 x 64, not split: 13.3 us of which the state's 16.8 MB take 4.
 //
 // A chunk with a value that is not finite is worked on step by step (chunks of one): a product with a zero weight
 // would carry it into steps before it and past flags.
@@ -719,7 +728,10 @@ struct DecayPlan {
     size_t factor_at, workspace; // bytes: where the factors stand, all
 };
 
-constexpr int DECAY_SHORT = 8;   // steps up to which the recurrence is walked
+// Steps up to which the recurrence is walked: a step is a chain of two barriers, where a chunk costs the same for one step
+// as for all of its own.  128 rows of 4 heads of 64 x 64: 4.9 us and 0.7 a step, a chunk 12; 64 rows of 16 heads of
+// 128 x 128: 22 us and 2.2 a step, a chunk 49 (bf16), 59 (fp32).
+constexpr int DECAY_SHORT = 8;
 
 static inline DecayPlan decay_plan(int dtype, int T, int B, int H, int dk, int dv)
 {

@@ -4,7 +4,7 @@
 //
 // Bound by memory: x in, y out, a few operations a value.  Where a row's values stay in registers between the statistics
 // and the result they travel once; mean and variance are always two passes over values that are held (differences to
-// the mean, squared), never a difference of sums.  Kernels, by shape (norm_launch):
+// the mean, squared), never a difference of sums.  Kernels, by shape (norm_plan):
 //   segment   points == 1: a group is a run of channels; a few lanes own it, sums are shuffles.
 //   resident  a row (or a slice of its groups) fits a workgroup's registers: read once, written once.
 //   split     larger rows: statistics of runs of points, then a second kernel that joins them and reads x again.
