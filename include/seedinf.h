@@ -457,7 +457,9 @@ const char* seed_op_last_error(void);
  *   state_in  [rows, heads, key_dim, value_dim] fp32 or NULL (zero)
  *   state_out the same shape; may be state_in itself, else must not overlap it
  *
- * out must not overlap q, k or v; state_out no other array.  1 <= key_dim,
+ * out, state_out and the workspace must not overlap any other array (but
+ * state_out may be state_in), out's rows not one another: one of its strides
+ * steps over a row, the other over all rows of the first.  1 <= key_dim,
  * value_dim <= 256, kv_heads divides heads.  steps == 0 copies the state (zero
  * where state_in is NULL); rows == 0 is a no-op.
  * Products of bf16 inputs are exact and added in fp32; the state is fp32

@@ -109,11 +109,18 @@ extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, con
     if (!decay || !state_out || (d->steps > 0 && (!q || !k || !v || !out)))
         return op_fail(SEED_ERR_INVALID_ARG, "q, k, v, decay, out and state_out are required");
     const size_t size = op_dtype_size(d->dtype);
-    if (!op_aligned(q, size) || !op_aligned(k, size) || !op_aligned(v, size) || !op_aligned(out, size) || !op_aligned(state_in, 4) || !op_aligned(state_out, 4))
+    if (!op_aligned(q, size) || !op_aligned(k, size) || !op_aligned(v, size) || !op_aligned(out, size) || !op_aligned(state_in, 4) || !op_aligned(state_out, 4) ||
+        !op_aligned(decay, 4) || !op_aligned(lengths, 4))
         return op_fail(SEED_ERR_INVALID_ARG, "an array is not aligned to its element");
     const size_t state_bytes = (size_t)d->rows * d->heads * d->key_dim * d->value_dim * sizeof(float);
     if (state_in != state_out && op_overlap(state_in, state_bytes, state_out, state_bytes))
         return op_fail(SEED_ERR_ALIASING, "state_out overlaps state_in without being it");
+    const struct { const void* p; size_t bytes; } small[] = {{decay, (size_t)d->heads * 4}, {done, (size_t)d->steps * d->rows}, {lengths, (size_t)d->rows * 4}};
+    for (const auto& a : small)
+        if (op_overlap(a.p, a.bytes, state_out, state_bytes)) return op_fail(SEED_ERR_ALIASING, "state_out overlaps decay, done or lengths");
+    const size_t need = seed_op_decay_workspace(d);
+    if (need && (op_overlap(workspace, need, state_in, state_bytes) || op_overlap(workspace, need, state_out, state_bytes)))
+        return op_fail(SEED_ERR_ALIASING, "the workspace overlaps a state");
     if (d->steps > 0) {
         const StridedArray arrays[] = {{out, d->out_step, d->out_row, (int64_t)d->heads * d->value_dim},
                                        {q, d->q_step, d->q_row, (int64_t)d->heads * d->key_dim},
@@ -123,12 +130,20 @@ extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, con
             if (a.p != out && strided_overlap(arrays[0], a, d->steps, d->rows, size)) return op_fail(SEED_ERR_ALIASING, "out overlaps q, k or v");
             const size_t extent = (size_t)((d->steps - 1) * a.step + (d->rows - 1) * a.row + a.width) * size;
             if (op_overlap(a.p, extent, state_out, state_bytes)) return op_fail(SEED_ERR_ALIASING, "state_out overlaps q, k, v or out");
+            if (need && op_overlap(a.p, extent, workspace, need)) return op_fail(SEED_ERR_ALIASING, "the workspace overlaps q, k, v or out");
+            if (a.p != out) continue;
+            if (op_overlap(out, extent, state_in, state_bytes)) return op_fail(SEED_ERR_ALIASING, "out overlaps state_in");
+            for (const auto& b : small)
+                if (op_overlap(out, extent, b.p, b.bytes)) return op_fail(SEED_ERR_ALIASING, "out overlaps decay, done or lengths");
         }
         if (out == q || out == k || out == v) return op_fail(SEED_ERR_ALIASING, "out overlaps q, k or v");
-        if ((d->steps > 1 && d->out_step < arrays[0].width) || (d->rows > 1 && d->out_row < arrays[0].width))
-            return op_fail(SEED_ERR_ALIASING, "out's strides make its rows overlap");
+        // out's rows lie apart: one of its strides steps over a whole row, the other over all rows of the first
+        const bool rows_outer = d->steps == 1 || (d->rows > 1 && d->out_row > d->out_step);
+        const int64_t w = arrays[0].width, so = rows_outer ? d->out_row : d->out_step, no = rows_outer ? d->rows : d->steps;
+        const int64_t si = rows_outer ? d->out_step : d->out_row, ni = rows_outer ? d->steps : d->rows;
+        if ((ni > 1 && si < w) || (no > 1 && so < (ni - 1) * si + w)) return op_fail(SEED_ERR_ALIASING, "out's strides make its rows overlap");
     }
-    if ((st = op_check_workspace(seed_op_decay_workspace(d), workspace, workspace_bytes)) != SEED_OK) return st;
+    if ((st = op_check_workspace(need, workspace, workspace_bytes)) != SEED_OK) return st;
     DecayArgs p{};
     p.q = q; p.k = k; p.v = v; p.decay = decay; p.done = done; p.lengths = lengths; p.s_in = state_in; p.out = out; p.s_out = state_out;
     p.q_t = d->q_step; p.q_b = d->q_row; p.k_t = d->k_step; p.k_b = d->k_row; p.v_t = d->v_step; p.v_b = d->v_row; p.o_t = d->out_step; p.o_b = d->out_row;
@@ -194,7 +209,10 @@ extern "C" seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t
         return op_fail(SEED_ERR_INVALID_ARG, "an array is not aligned to its element");
     if ((x != out && op_overlap(x, bytes, out, bytes)) || op_overlap(weight, (size_t)channels * 4, out, bytes) || op_overlap(bias, (size_t)channels * 4, out, bytes))
         return op_fail(SEED_ERR_ALIASING, "out overlaps x without being it, or weight or bias");
-    if ((st = op_check_workspace(seed_op_group_norm_workspace(dtype, rows, points, channels, groups), workspace, workspace_bytes)) != SEED_OK) return st;
+    const size_t need = seed_op_group_norm_workspace(dtype, rows, points, channels, groups), params = (size_t)channels * 4;
+    if (need && (op_overlap(workspace, need, x, bytes) || op_overlap(workspace, need, out, bytes) || op_overlap(workspace, need, weight, params) || op_overlap(workspace, need, bias, params)))
+        return op_fail(SEED_ERR_ALIASING, "the workspace overlaps an array");
+    if ((st = op_check_workspace(need, workspace, workspace_bytes)) != SEED_OK) return st;
     int vec = (int)(16 / size);
     while (!op_aligned(x, vec * size) || !op_aligned(out, vec * size)) vec /= 2;
     const NormPlan plan = norm_plan(rows, points, channels, groups, (int)size, vec);

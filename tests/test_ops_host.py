@@ -138,3 +138,43 @@ def test_binding_refuses_host_tensors():
         seedinf.group_norm(x, 1)
     with pytest.raises(TypeError):
         seedinf.decay_attention(x, x, x, x)
+
+
+@pytest.mark.parametrize("kw", [dict(out=5 * A), dict(out=4 * A), dict(done=6 * A), dict(lengths=6 * A + 64), dict(lengths=7 * A), dict(decay=7 * A + 16), dict(done=7 * A)])
+def test_decay_refuses_outputs_over_small_inputs(lib, kw):
+    st, msg = decay_call(lib, decay_desc(), **kw)
+    assert st == ALIASING and "overlap" in msg
+    for name in ("decay", "lengths"):
+        st, msg = decay_call(lib, decay_desc(), **{name: A + 2})
+        assert st == INVALID and "aligned" in msg, name
+
+
+@pytest.mark.parametrize("step,row,ok", [(128, 64, True), (64, 4096 * 64, True), (200, 65, True), (64, 64, False), (96, 64, False), (64, 4096 * 64 - 1, False),
+                                         (63, 1 << 20, False), (0, 64, False), (127, 64, False)])
+def test_decay_refuses_outputs_whose_rows_meet(lib, step, row, ok):
+    """4096 steps of 2 rows of 64 elements: which strides keep them apart (accepted ones are refused for the missing workspace, so nothing runs)."""
+    desc = decay_desc(steps=4096, rows=2, heads=1, kv_heads=1, key_dim=64, value_dim=64, out_step=step, out_row=row)
+    st, msg = decay_call(lib, desc, **FAR)
+    assert (st == INVALID and "workspace" in msg) if ok else (st == ALIASING and "rows overlap" in msg)
+
+
+FAR = dict(q=1 << 30, k=2 << 30, v=3 << 30, out=4 << 30, state=5 << 30, state_out=6 << 30)
+
+
+def test_workspaces_must_not_overlap(lib):
+    desc = decay_desc(steps=4096, rows=1, heads=1, kv_heads=1, key_dim=64, value_dim=64)
+    n = lib.seed_op_decay_workspace(C.byref(desc))
+    assert n > 0
+    far = FAR
+    for name, at in far.items():
+        st, msg = decay_call(lib, desc, **far, ws=at, n=n)
+        assert st == ALIASING and "workspace" in msg, name
+    st, msg = decay_call(lib, desc, **far, ws=7 << 30, n=n - 1)
+    assert st == INVALID and "workspace" in msg
+    sizes = dict(dtype=0, rows=1, points=100000, channels=32, groups=4)
+    n = lib.seed_op_group_norm_workspace(*sizes.values())
+    assert n > 0
+    a = dict(sizes, x=1 << 30, weight=2 << 30, bias=3 << 30, eps=1e-5, act=0, out=4 << 30, ws=None, n=n)
+    for name in ("x", "weight", "bias", "out"):
+        assert lib.seed_op_group_norm(*dict(a, ws=a[name]).values(), None) == ALIASING, name
+    assert lib.seed_op_group_norm(*a.values(), None) == INVALID
