@@ -449,7 +449,8 @@ const char* seed_op_last_error(void);
  *          A row's heads are dense; steps and rows have strides of their own
  *          (elements, not negative), so that the three may be parts of one
  *          projection's output and the order may be time- or batch-major.
- *   decay  [heads] fp32, usually in [0, 1]
+ *   decay  [heads] fp32, of magnitude at most 1 (powers of a larger one over
+ *          64 steps have to be finite)
  *   done   [steps, rows] uint8, dense, or NULL
  *   lengths [rows] int32 or NULL (all `steps`): row b has lengths[b] steps
  *          (clamped to 0 .. steps); what lies behind them is neither read nor
@@ -460,7 +461,7 @@ const char* seed_op_last_error(void);
  * out, state_out and the workspace must not overlap any other array (but
  * state_out may be state_in), out's rows not one another: one of its strides
  * steps over a row, the other over all rows of the first.  1 <= key_dim,
- * value_dim <= 256, kv_heads divides heads.  steps == 0 copies the state (zero
+ * value_dim <= 256, kv_heads divides heads, rows * heads <= 2^21.  steps == 0 copies the state (zero
  * where state_in is NULL); rows == 0 is a no-op.
  * Products of bf16 inputs are exact and added in fp32; the state is fp32
  * throughout.  A value that is not finite reaches the steps behind it, up to
@@ -494,7 +495,8 @@ seed_status_t seed_op_decay(const seed_decay_t* desc, const void* q, const void*
  *   weight, bias   [channels] fp32, each may be NULL
  *   activation     SEED_ACT_NONE, SEED_ACT_RELU or SEED_ACT_SILU (v * sigmoid(v))
  *
- * groups divides channels, eps >= 0.  rows == 0 or points == 0 is a no-op.
+ * groups divides channels, eps >= 0, points * channels < 2^31, rows * groups <=
+ * 2^23.  rows == 0 or points == 0 is a no-op.
  */
 size_t seed_op_group_norm_workspace(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups);
 seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups,
@@ -526,7 +528,7 @@ seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, in
  *                (0 if greedy, -inf without a choice), or NULL
  *
  * A logit of -inf or NaN is no choice; equal logits of +inf share the mass.
- * 1 <= choices <= SEED_SAMPLE_MAX_CHOICES; rows == 0 is a no-op.
+ * 1 <= choices <= SEED_SAMPLE_MAX_CHOICES, rows <= 2^21; rows == 0 is a no-op.
  */
 #define SEED_SAMPLE_MAX_CHOICES (1 << 24)
 size_t seed_op_sample_workspace(int32_t dtype, int32_t rows, int32_t choices);

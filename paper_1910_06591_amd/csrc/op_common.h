@@ -40,6 +40,10 @@ static inline hipError_t op_allow_lds(const void* kernel, size_t bytes, std::ato
     return e;
 }
 
+// What seed_op_sample checks of its arguments (ops.hip), for a step that samples behind its heads.
+seed_status_t op_sample_check(int32_t dtype, int32_t rows, int32_t choices, int64_t row_stride, const void* logits, const float* uniforms,
+                              const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* token_out, float* logprob_out);
+
 static inline size_t op_dtype_size(int32_t dtype) { return dtype == SEED_DTYPE_FP32 ? 4 : 2; }
 
 }  // namespace seedinf

@@ -238,10 +238,10 @@ extern "C" size_t seed_op_sample_workspace(int32_t dtype, int32_t rows, int32_t 
     return 0;
 }
 
-extern "C" seed_status_t seed_op_sample(int32_t dtype, int32_t rows, int32_t choices, int64_t row_stride, const void* logits,
+// Everything that seed_op_sample refuses.
+seed_status_t seedinf::op_sample_check(int32_t dtype, int32_t rows, int32_t choices, int64_t row_stride, const void* logits,
                                         const float* uniforms, const float* temperature, const int32_t* top_k, const float* top_p,
-                                        const float* min_p, int32_t* token_out, float* logprob_out, void* workspace,
-                                        size_t workspace_bytes, void* hip_stream)
+                                        const float* min_p, int32_t* token_out, float* logprob_out)
 {
     seed_status_t st = sample_check(dtype, rows, choices);
     if (st != SEED_OK) return st;
@@ -258,6 +258,16 @@ extern "C" seed_status_t seed_op_sample(int32_t dtype, int32_t rows, int32_t cho
     if (!op_aligned(token_out, 4) || !op_aligned(logprob_out, 4)) return op_fail(SEED_ERR_INVALID_ARG, "an array is not aligned to its element");
     if (op_overlap(logits, bytes, token_out, row4) || op_overlap(logits, bytes, logprob_out, row4) || op_overlap(token_out, row4, logprob_out, row4))
         return op_fail(SEED_ERR_ALIASING, "an output overlaps an input or the other output");
+    return SEED_OK;
+}
+
+extern "C" seed_status_t seed_op_sample(int32_t dtype, int32_t rows, int32_t choices, int64_t row_stride, const void* logits,
+                                        const float* uniforms, const float* temperature, const int32_t* top_k, const float* top_p,
+                                        const float* min_p, int32_t* token_out, float* logprob_out, void* workspace,
+                                        size_t workspace_bytes, void* hip_stream)
+{
+    seed_status_t st = op_sample_check(dtype, rows, choices, row_stride, logits, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out);
+    if (st != SEED_OK || rows == 0) return st;
     if ((st = op_check_workspace(seed_op_sample_workspace(dtype, rows, choices), workspace, workspace_bytes)) != SEED_OK) return st;
     SampleArgs p{logits, row_stride, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, rows, choices, sample_shift(choices)};
     const hipError_t e = dtype == SEED_DTYPE_FP32 ? sample_launch<float>(p, (hipStream_t)hip_stream) : sample_launch<__bf16>(p, (hipStream_t)hip_stream);

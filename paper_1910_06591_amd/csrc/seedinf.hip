@@ -18,6 +18,7 @@
 #include "kernels_fp32.h"
 #include "kernels_heads.h"
 #include "bf16_path.h"
+#include "op_common.h"
 
 using namespace seedinf;
 
@@ -563,6 +564,11 @@ static seed_status_t step_impl(seed_infer_t* h, int32_t B, const uint8_t* obs,
         if (sampled && epsilon) return fail(SEED_ERR_INVALID_ARG, "epsilon and sample_uniforms are two ways to select: give one");
         if (ext->struct_size == sizeof(seed_step_ext_t) && !sampled && (ext->temperature || ext->top_k || ext->top_p || ext->min_p))
             return fail(SEED_ERR_INVALID_ARG, "temperature, top_k, top_p and min_p need sample_uniforms");
+        if (sampled) {
+            const seed_status_t st = op_sample_check(SEED_DTYPE_FP32, B, a.num_actions, a.num_actions, logits_out, ext->sample_uniforms, ext->temperature,
+                                                     ext->top_k, ext->top_p, ext->min_p, action_out, nullptr);
+            if (st != SEED_OK) return fail(st, seed_op_last_error());
+        }
     }
     if (rec) {
         size_t nb = (size_t)B * a.lstm_units * sizeof(float);

@@ -120,3 +120,24 @@ def test_step_refuses_two_selections_and_accepts_the_shorter_struct():
     assert st == 0, msg
     assert all(torch.equal(out[k], want[k]) for k in want)
     net.close()
+
+
+def test_step_refuses_sampling_arguments_before_anything_runs():
+    """Uniforms that are the actions' own memory, top_k at an odd address: the outputs stay as they were."""
+    import torch
+    cfg = wl.CONFIGS["C1"]
+    B = 4
+    net = seedinf.SeedInfer(seedinf.make_arch(cfg, max_batch=B), wl.make_weights(cfg))
+    batch = to_device(wl.make_batch(cfg, B))
+    out = {k: torch.empty_like(v) for k, v in net.step(**batch).items()}
+    for v in out.values():
+        v.fill_(7)
+    u = torch.rand(B, device="cuda")
+    for fields, status in (((out["action"].data_ptr(), None, None, None, None), 4), ((u.data_ptr(), None, u.data_ptr() + 2, None, None), 1)):
+        ext = seedinf.SeedStepExt(C.sizeof(seedinf.SeedStepExt), None, None, None, *fields)
+        st, _ = net.step_ext_raw(B, batch["obs"].data_ptr(), None, None, None, None, None, ext, out["action"].data_ptr(),
+                                 out["logits"].data_ptr(), out["value"].data_ptr(), None, None, out["probs"].data_ptr())
+        torch.cuda.synchronize()
+        assert st == status
+        assert all((v == 7).all() for v in out.values())
+    net.close()
