@@ -465,8 +465,15 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
             });
             __syncthreads();
             cands = l.n;
+            __syncthreads();                                 // (read by all before the next tiles add to it)
             if (cands > CAP) break;
-            if (cands > 3 * CAP / 8 || end == tiles) {         // the centre at the largest so far, the cut anew, and out with what is below it
+            if (cands <= 3 * CAP / 8) {
+                if (end < tiles) continue;
+                top = -INFINITY;                             // few enough at the end: the centre at the largest is all that is wanted
+                for (int i = tid; i < cands; i += NT) top = fmaxf(top, value(cand[i]));
+                top = largest(top);
+                bins.centre = (double)top;
+            } else {                                         // the centre at the largest so far, the cut anew, and out with what is below it
                 uint64_t mine[CAP / NT];
                 top = -INFINITY;
 #pragma unroll
@@ -490,6 +497,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
                 for (int j = 0; j < CAP / NT; ++j) if (mine[j] && value(mine[j]) >= cut) cand[atomicAdd(&l.n, 1)] = mine[j];
                 __syncthreads();
                 cands = l.n;
+                __syncthreads();
             }
         }
         listed = cands <= CAP && top != INFINITY;
