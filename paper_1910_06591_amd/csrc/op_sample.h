@@ -13,7 +13,7 @@
 //          by one instead, by radix searches over the row (sample_find; 64 x 50001 within a hundredth of a temperature:
 //          190 us, with top-p 290, where spread logits take 40).
 // What bounds a row: the operations in 64 bits and the LDS additions of the first pass, then some twenty dependent phases
-// of 1 - 3 us; few rows leave most compute units idle (64 x 50001 bf16: 44 - 53 us; 4 x 32000 fp32, top-k 50: 26 us).  256 rows of
+// of 1 - 3 us; few rows leave most compute units idle (64 x 50001 bf16: 44 - 53 us; 4 x 32000 fp32, top-k 50: 24 us).  256 rows of
 // 131072 fp32, top-k 1000: 70 us, 1.9 TB/s.  4096 rows of 18: 5.4 us, a launch's own time.
 #pragma once
 #include <atomic>
