@@ -130,10 +130,10 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
 // tiles are the state's in an order (decay_row) in which a lane's values of two tiles are the eight consecutive key
 // elements that a bf16 operand wants, so S is an operand as it stands.
 //
-// Roundings: bf16 inputs are operands as they are.  What is computed between the products is split into bf16 parts whose
-// sum it is: scores and state into two (2^-16 of the value is lost, small beside the output's own 2^-8), the weighted
-// values of the state's update into three (nothing is lost: the state is fp32) or, where it feeds outputs only, two (long
-// case: 247 us with three, 236 with two).  fp32 inputs use the fp32 matrix instructions.
+// Roundings: bf16 inputs are operands as they are.  What is computed between the products (scores, the state as an operand,
+// the weighted values of its update) is fp32 and is split into three bf16 parts whose sum it is, 24 bits, so that nothing
+// is lost (in two parts outputs were 1.0e-4 of their norm off; 4 prompts of up to 4001 steps: 132 us, with two parts 119;
+// 32768 steps of 16 heads: 255 and 232).  fp32 inputs use the fp32 matrix instructions.
 //
 // What bounds it: not the bytes (32768 steps of 16 heads of 128 x 128, bf16: 537 MB are 100 us), but a chunk's phases,
 // each of which waits for the one before it: LDS writes of keys and values with their steps side by side, scores, their
@@ -227,7 +227,7 @@ template <int R> __device__ __forceinline__ uint32_t decay_operand(uint32_t x, i
 
 template <class T, int DK, int DVT, bool OUT> struct DecayLds {
     static constexpr int C = DecayMma<T>::C;
-    static constexpr int KROW = DK * (int)sizeof(T), CROW = C * (int)sizeof(T), PARTS = sizeof(T) == 4 ? 1 : 2;      // bytes a row
+    static constexpr int KROW = DK * (int)sizeof(T), CROW = C * (int)sizeof(T), PARTS = sizeof(T) == 4 ? 1 : 3;      // bytes a row
     static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (KROW > PARTS * CROW ? C * KROW : PARTS * C * CROW) : 0;
     // queries; keys, later the scores' parts; keys and values with their steps side by side; tables
     static constexpr int Q = 0, K = NQ, KT = K + NK, VT = KT + DK * CROW, END = VT + DVT * CROW;
@@ -521,9 +521,11 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                     else {
                         char* const to = ldsk + decay_at<CROW>(i, 2 * jt + (lg >> 1)) + 8 * (lg & 1);
                         const bf16x4 hi = to_bf16x4(f);
-                        const floatx4 hf = to_floatx4(hi);
+                        const floatx4 rest = f - to_floatx4(hi);
+                        const bf16x4 mid = to_bf16x4(rest);
                         *(bf16x4*)to = hi;
-                        *(bf16x4*)(to + C * CROW) = to_bf16x4(f - hf);
+                        *(bf16x4*)(to + C * CROW) = mid;
+                        *(bf16x4*)(to + 2 * C * CROW) = to_bf16x4(rest - to_floatx4(mid));
                     }
                 }
             }
@@ -534,29 +536,28 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                 for (int n = 0; n < NT; ++n) acc[it2][n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int d = 0; d < DK / KS; ++d) {
-                Frag fq[IT], s0[NT], s1[NT];
+                Frag fq[IT];
+                float x[NT][8];                              // what is left of the state
 #pragma unroll
                 for (int it2 = 0; it2 < IT; ++it2) fq[it2] = *(const Frag*)(ldsq + decay_operand<KROW>(xk, it2, d));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if constexpr (sizeof(T) == 4) s0[n] = S[d][n];
-                    else {
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = S[2 * d + (e >> 2)][n][e & 3];
-                        s0[n] = decay_split8(x);
-                        s1[n] = decay_round8(x);
-                    }
-                }
-#pragma unroll
-                for (int it2 = 0; it2 < IT; ++it2)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(s0[n], fq[it2], acc[it2][n]);
                 if constexpr (sizeof(T) == 2)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[n][e] = S[2 * d + (e >> 2)][n][e & 3];
+#pragma unroll
+                for (int part = 0; part < L::PARTS; ++part) {
+                    Frag fs[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        if constexpr (sizeof(T) == 4) fs[n] = S[d][n];
+                        else fs[n] = part < 2 ? decay_split8(x[n]) : decay_round8(x[n]);
+                    }
 #pragma unroll
                     for (int it2 = 0; it2 < IT; ++it2)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(s1[n], fq[it2], acc[it2][n]);
+                        for (int n = 0; n < NT; ++n) acc[it2][n] = M::mma(fs[n], fq[it2], acc[it2][n]);
+                }
                 __builtin_amdgcn_sched_barrier(0);           // (the state's parts are made where they are used)
             }
 #pragma unroll
@@ -584,11 +585,10 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
             for (int ks = 0; ks < JS; ++ks) vt[n][ks] = *(const Frag*)(ldsvt + decay_operand<CROW>(xc, n, ks) + wave * NT * 16 * CROW);
 
         if constexpr (OUT) {
-            constexpr int PARTS = sizeof(T) == 4 ? 1 : 2;
 #pragma unroll
             for (int ks = 0; ks < JS; ++ks)
 #pragma unroll
-                for (int part = 0; part < PARTS; ++part)
+                for (int part = 0; part < L::PARTS; ++part)
 #pragma unroll
                     for (int it2 = 0; it2 < IT; ++it2) {
                         if (ks * KS > 16 * it2) continue;
@@ -639,10 +639,7 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
         }
 #pragma unroll
         for (int ks = 0; ks < JS; ++ks) {
-            constexpr int W = sizeof(T) == 4 ? 1 : 3;
-            // a split time axis has its final state from the segments' own: this one only feeds outputs, two parts do
-            const bool three = !OUT || !split;
-            Frag w[W][NT];
+            Frag w[L::PARTS][NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const floatx4 wa = *(const floatx4*)(wend + ks * KS + FE * lg);
@@ -653,10 +650,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                     float x[8] = {bf16_lo_f32(u.x) * wa[0], bf16_hi_f32(u.x) * wa[1], bf16_lo_f32(u.y) * wa[2], bf16_hi_f32(u.y) * wa[3],
                                   bf16_lo_f32(u.z) * wb[0], bf16_hi_f32(u.z) * wb[1], bf16_lo_f32(u.w) * wb[2], bf16_hi_f32(u.w) * wb[3]};
                     w[0][n] = decay_split8(x);
-                    if (three) {
-                        w[1][n] = decay_split8(x);
-                        w[2][n] = decay_round8(x);
-                    } else w[1][n] = decay_round8(x);
+                    w[1][n] = decay_split8(x);
+                    w[2][n] = decay_round8(x);
                 }
             }
 #pragma unroll
@@ -665,12 +660,11 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
 #pragma unroll
                 for (int x = 0; x < 4; ++x) fk[x] = *(const Frag*)(ldskt + decay_operand<CROW>(xc, m + x, ks));
 #pragma unroll
-                for (int y = 0; y < W; ++y)
-                    if (y < 2 || three)
+                for (int y = 0; y < L::PARTS; ++y)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
+                    for (int x = 0; x < 4; ++x)
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) S[m + x][n] = M::mma(fk[x], w[y][n], S[m + x][n]);
+                        for (int n = 0; n < NT; ++n) S[m + x][n] = M::mma(fk[x], w[y][n], S[m + x][n]);
             }
         }
         __syncthreads();                                     // everything staged is read

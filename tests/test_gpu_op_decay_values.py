@@ -1,0 +1,82 @@
+"""seed_op_decay on the GPU at values where arithmetic of fewer bits, another order of operations or a product that the
+recurrence never forms would show."""
+import numpy as np
+import pytest
+
+from paper_1910_06591_amd import seedinf
+from tests import ops_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def run(q, k, v, decay, dtype="bf16", **kw):
+    """Arrays of the host in, out and state as fp64 arrays of the host."""
+    import torch
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().to(dt)  # noqa: E731
+    kw = {n: torch.from_numpy(np.ascontiguousarray(x)).cuda() if isinstance(x, np.ndarray) else x for n, x in kw.items()}
+    out, state = seedinf.decay_attention(dev(q), dev(k), dev(v), torch.tensor(decay, dtype=torch.float32, device="cuda"), **kw)
+    return out.double().cpu().numpy(), state.double().cpu().numpy()
+
+
+def test_scores_keep_24_bits():
+    """Two steps whose scores are integers of up to 22 bits and whose values are 1 and -1: an output is the scores' small
+    difference.  Every product and sum is an integer below 2^24 and the outputs are of 8 bits at most, so nothing rounds."""
+    rng = np.random.default_rng(0)
+    T, d = 64, 64
+    q, k, v = np.zeros((T, 1, 1, d)), np.zeros((T, 1, 1, d)), np.zeros((T, 1, 1, d))
+    q[:, 0, 0] = rng.integers(128, 256, (T, d))
+    q[:, 0, 0, 7] = rng.integers(1, 100, T)
+    k[3, 0, 0] = rng.integers(128, 255, d)
+    k[5, 0, 0] = k[3, 0, 0]
+    k[3, 0, 0, 7] += 1                                   # (127 .. 255: of 8 bits)
+    v[3], v[5] = 1, -1
+    out, _ = run(q, k, v, [1.0])
+    want = np.zeros_like(q)
+    want[3:5] = np.sum(q[3:5] * k[3], -1, keepdims=True)
+    want[5:] = q[5:, :, :, 7:8]
+    assert (out[:3] == 0).all() and (out[5:] == want[5:]).all(), np.abs(out[5:] - want[5:]).max()
+    assert (np.abs(out[3:5] - want[3:5]) <= ref.UBF * want[3:5]).all()
+
+
+@pytest.mark.parametrize("dk", [64, 100, 256])
+def test_the_state_keeps_24_bits(dk):
+    """A state of integers of up to 22 bits, and queries that take one of its rows from another that is all but equal."""
+    rng = np.random.default_rng(1)
+    T, dv = 128, 64
+    q, k, v = np.zeros((T, 1, 1, dk)), np.zeros((T, 1, 1, dk)), np.zeros((T, 1, 1, dv))
+    row = rng.integers(128, 255, 64)
+    k[:64, 0, 0] = row[:, None]
+    at = rng.integers(0, 64, dk)                         # where row d of the state has 1 more
+    for d in range(1, dk):
+        k[at[d], 0, 0, d] += 1
+    v[:64, 0, 0] = rng.integers(128, 256, (64, dv))
+    for t in range(64, T):
+        d = 1 + (t * 5) % (dk - 1)
+        q[t, 0, 0, d], q[t, 0, 0, 0] = 1, -1
+    out, state = run(q, k, v, [1.0])
+    S = np.einsum("tk,tv->kv", k[:64, 0, 0], v[:64, 0, 0])
+    assert S.max() < 2 ** 24 and (state[0, 0] == S).all()
+    assert (out[64:, 0, 0] == q[64:, 0, 0] @ S).all()
+
+
+def test_the_update_keeps_24_bits_where_the_axis_is_split():
+    """Weights g^2 and g^3 of 16 and 24 bits (g = n / 256) and keys that all but cancel them.  An entry of the state is
+    k g^3 - k' g^2: two roundings of a product or sum and one of the power behind it, then the query's power and the
+    output: 4 roundings of 2^-24 of the terms, and the output's own."""
+    T, d = 1024, 64
+    heads = [231, 239, 241, 247, 251, 253]
+    H = len(heads)
+    q, k, v = np.zeros((T, 1, H, d)), np.zeros((T, 1, H, d)), np.zeros((T, 1, H, d))
+    for h, n in enumerate(heads):
+        a, b = np.meshgrid(np.arange(128, 256), np.arange(100, 256), indexing="ij")
+        diff = np.abs(a * n - b * 256)
+        best = np.argsort(np.where(diff > 0, diff, 1 << 30), axis=None)[:d]
+        k[60, 0, h], k[61, 0, h] = a.flat[best], b.flat[best]
+    v[60], v[61] = 1, -1
+    for i in range(d):
+        q[64 + i, 0, :, i] = 1
+    g = np.array(heads) / 256
+    out, _ = run(q, k, v, g)
+    want, _, mag, _ = ref.decay(q, k, v, g)
+    assert (np.abs(out - want) <= 4 * ref.U32 * mag + ref.UBF * np.abs(want)).all(), np.max(np.abs(out - want)[64:128] / mag[64:128]) / ref.U32
