@@ -84,6 +84,7 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (ty + 16 * r >= p.dk) continue;              // (a row that is not there: 0 times an infinite value)
             const float kr = sk[ty + 16 * r], qr = sq[ty + 16 * r];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

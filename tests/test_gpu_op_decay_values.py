@@ -80,3 +80,57 @@ def test_the_update_keeps_24_bits_where_the_axis_is_split():
     out, _ = run(q, k, v, g)
     want, _, mag, _ = ref.decay(q, k, v, g)
     assert (np.abs(out - want) <= 4 * ref.U32 * mag + ref.UBF * np.abs(want)).all(), np.max(np.abs(out - want)[64:128] / mag[64:128]) / ref.U32
+
+
+def same(got, want, tol):
+    """NaN where the definition has NaN, its infinities, and finite values within the tolerance."""
+    assert np.array_equal(np.isnan(got), np.isnan(want)), "NaN in other places"
+    inf = np.isinf(want)
+    assert np.array_equal(np.isinf(got), inf) and (got[inf] == want[inf]).all(), "infinities in other places"
+    fine = np.isfinite(want)
+    assert (np.abs(got - want, where=fine, out=np.zeros_like(want))[fine] <= tol[fine]).all()
+
+
+def values(T, B, H, dk, dv, seed):
+    """q and k positive, so that an infinite value is one in every sum that it enters."""
+    rng = np.random.default_rng(seed)
+    q, k = 0.1 + rng.random((T, B, H, dk)), (0.1 + rng.random((T, B, H, dk))) / dk
+    return rng, q, k, rng.standard_normal((T, B, H, dv)), rng.uniform(0.5, 0.999, H).astype(np.float32).astype(np.float64)
+
+
+def rounded(x, dtype):
+    """The values that arrive as `dtype`."""
+    import torch
+    return torch.from_numpy(np.asarray(x, np.float32)).to(torch.float32 if dtype == "fp32" else torch.bfloat16).double().numpy()
+
+
+def check_not_finite(T, dk, dv, dtype, seed, done=None, **inputs):
+    """Infinite keys, values, queries and states against the definition in 64 bits."""
+    B, H = 4, 2
+    rng, q, k, v, g = values(T, B, H, dk, dv, seed)
+    s = rng.standard_normal((B, H, dk, dv)).astype(np.float32)
+    at = T // 3
+    k[at, 0, 0, dk // 2] = np.inf
+    v[at, 1, 1, dv // 2] = -np.inf
+    q[at, 2, 0, dk - 1] = np.inf
+    q[T - 1, 2, 1, 0] = np.nan
+    s[3, 0, dk // 3, dv // 3] = np.inf
+    if done is not None:
+        done = (rng.random((T, B)) < done).astype(np.uint8)
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    with np.errstate(invalid="ignore"):
+        ro, rs, mag, A = ref.decay(q, k, v, g, s, done)
+        tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, T, dk, dtype == "bf16")
+        out, state = run(q, k, v, g, dtype, state=s, done=done, **inputs)
+        same(state, rs, tol_s)
+        same(out, ro, tol_o)
+
+
+DIMS = [(8, 20), (64, 64), (100, 36), (33, 17), (128, 128), (130, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [1, 7])
+@pytest.mark.parametrize("dk,dv", DIMS)
+def test_infinities_of_few_steps_are_the_definitions(dk, dv, T, dtype):
+    check_not_finite(T, dk, dv, dtype, dk + T)
