@@ -134,3 +134,42 @@ DIMS = [(8, 20), (64, 64), (100, 36), (33, 17), (128, 128), (130, 256)]
 @pytest.mark.parametrize("dk,dv", DIMS)
 def test_infinities_of_few_steps_are_the_definitions(dk, dv, T, dtype):
     check_not_finite(T, dk, dv, dtype, dk + T)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [9, 70, 1100])
+@pytest.mark.parametrize("dk,dv", DIMS[:4])
+def test_infinite_keys_and_values_of_many_steps(dk, dv, T, dtype):
+    """As above in chunks, in segments of the axis (1100 steps), and where heads are not whole 16 bytes.  The state that
+    came in is finite, and so are the queries of the steps that the values reach."""
+    B, H = 3, 2
+    rng, q, k, v, g = values(T, B, H, dk, dv, T + dk)
+    s = rng.standard_normal((B, H, dk, dv)).astype(np.float32)
+    done = np.zeros((T, B), np.uint8)
+    at, end = T // 3, T // 3 + 3
+    k[at, 0, 0, dk // 2] = np.inf
+    v[at + 1, 1, 1, dv // 2] = -np.inf
+    v[at + 1, 2, 0, 0] = np.nan
+    done[end] = 1
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    with np.errstate(invalid="ignore"):
+        ro, rs, mag, A = ref.decay(q, k, v, g, s, done)
+        tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, T, dk, dtype == "bf16")
+        out, state = run(q, k, v, g, dtype, state=s, done=done)
+        same(state, rs, tol_s)
+        same(out, ro, tol_o)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [1100])
+def test_an_infinite_state_outlives_powers_that_are_zero(T, dtype):
+    """A key that is infinite in the first step, decays whose powers over 64 steps are no numbers any more: the state that
+    comes back is infinite, of the sign that its steps give it."""
+    rng, q, k, v, _ = values(T, 1, 2, 64, 64, T)
+    k[0, 0, :, 5] = np.inf
+    g = np.array([0.01, -0.01], np.float32).astype(np.float64)
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    with np.errstate(invalid="ignore"):
+        ro, rs, mag, A = ref.decay(q, k, v, g)
+        _, state = run(q, k, v, g, dtype)
+        same(state, rs, ref.decay_tolerance(ro, mag, rs, A, T, 64, dtype == "bf16")[1])
