@@ -463,9 +463,13 @@ const char* seed_op_last_error(void);
  * steps over a row, the other over all rows of the first.  1 <= key_dim,
  * value_dim <= 256, kv_heads divides heads, rows * heads <= 2^21.  steps == 0 copies the state (zero
  * where state_in is NULL); rows == 0 is a no-op.
- * Products of bf16 inputs are exact and added in fp32; the state is fp32
- * throughout.  A value that is not finite reaches the steps behind it, up to
- * the next step whose done is set, and nothing else.
+ * Products of bf16 inputs are exact and added in fp32; the state and what is
+ * computed between the products are fp32 throughout.  A value that is not
+ * finite reaches what the recurrence carries it to (the steps behind it, up to
+ * the next step whose done is set) and nothing else, an infinity as one; from
+ * the first such value on, or where a query times a key or the state leaves
+ * fp32's range, a row's head is worked on step by step, at a few microseconds a
+ * step.
  */
 typedef struct seed_decay {
     uint32_t struct_size;                    /* = sizeof(seed_decay_t) */

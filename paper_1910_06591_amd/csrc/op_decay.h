@@ -143,9 +143,11 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
 // of the states 19, the outputs 135; 4 prompts of up to 4001 steps in 8 segments: 37 + 17 + 64; fp32, 32 steps of 128 rows
 // of 4 heads of 64 x 64, not split: 13.3 us of which the state's 16.8 MB take 4.
 //
-// From a chunk with a key or value that is not finite on, a workgroup walks its steps as the recurrence says, on the state in
-// memory.  The products would carry such a value into steps before it and past flags (zero times infinity), and the parts of
-// an infinity are an infinity and NaN.  (It does not come back to chunks: with the state in accumulators on both sides of a
+// From a chunk on in which a key, a value, a score or a query times the state is not finite, a workgroup walks its steps as
+// the recurrence says, on the state in memory.  The products would carry such a value into steps before it and past flags
+// (zero times infinity), the parts of an infinity are an infinity and NaN, and a score is a product that the recurrence never
+// forms: of a large query with a later key, too.  What is not finite in queries and in the state shows in their products.
+// (It does not come back to chunks: with the state in accumulators on both sides of a
 // walk, 32768 steps of 16 heads of 128 x 128 took 281 us in place of 271.)
 
 template <class T> struct DecayMma;
@@ -234,7 +236,7 @@ template <class T, int DK, int DVT, bool OUT> struct DecayLds {
     static constexpr int NQ = OUT ? C * KROW : 0, NK = OUT ? (KROW > PARTS * CROW ? C * KROW : PARTS * C * CROW) : 0;
     // queries; keys, later the scores' parts; keys and values with their steps side by side; tables
     static constexpr int Q = 0, K = NQ, KT = K + NK, VT = KT + DK * CROW, END = VT + DVT * CROW;
-    static constexpr size_t BYTES = (size_t)END + (2 * C + 8) * sizeof(float) + 16 + (OUT ? (C + 4 + 512) * sizeof(float) : 0);
+    static constexpr size_t BYTES = (size_t)END + (2 * C + 8) * sizeof(float) + 32 + (OUT ? (C + 4 + 512) * sizeof(float) : 0);
     static constexpr int RESIDENT = BYTES <= 80 * 1024 ? 2 : 1;          // workgroups a compute unit
 };
 
@@ -305,8 +307,8 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
     char* const ldsq = decay_lds + L::Q; char* const ldsk = decay_lds + L::K; char* const ldskt = decay_lds + L::KT; char* const ldsvt = decay_lds + L::VT;
     float* const pw = (float*)(decay_lds + L::END);          // powers 0 .. C
     float* const wend = pw + C + 4;                          // weight of step j in the state behind the chunk
-    uint64_t* const flags = (uint64_t*)(wend + C + 4);       // [0]: steps with a flag, [1]: a value is not finite
-    float* const reach = (float*)(flags + 2);                // OUT: scale times power i + 1: what step i sees of the state
+    uint64_t* const flags = (uint64_t*)(wend + C + 4);       // [0]: steps with a flag, [1]: a value is not finite, [2]: a score or query times state is not
+    float* const reach = (float*)(flags + 4);                // OUT: scale times power i + 1: what step i sees of the state
     floatx4* const near = (floatx4*)(reach + C + 4);         // OUT: scale times the powers between a lane's steps of two tiles, see below
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 15, lg = lane >> 4;
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
     float factor = 1.0f, cut = 0.0f;                         // of the segment so far
     int t0 = begin, c = min(C, end - begin);
     if (c > 0) { fetch_q(t0, c); fetch(t0, c); }
-    if (tid == 0) flags[1] = 0;
+    if (tid == 0) flags[1] = flags[2] = 0;
     __syncthreads();                                         // the table of powers
     while (c > 0) {
         stage(c);
@@ -525,6 +527,13 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
             }
             __syncthreads();                                 // keys are read: scores take their place
             if (nc > 0) fetch(next, nc);                     // on its way while the rest is multiplied
+            // NaN if a score, or below a query times the state, is not finite.  (Twice the score: the nearest bf16 of a finite
+            // one may be infinite, too.)
+            float none = 0.0f;
+#pragma unroll
+            for (int x = 0; x < SC; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) none = fmaf(sc[x][r] + sc[x][r], 0.0f, none);
             {
                 const int i = 16 * it + ln;
                 const floatx4 same = near[2 * lane], before = near[2 * lane + 1];
@@ -597,6 +606,13 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
                 __builtin_amdgcn_sched_barrier(0);           // (the state's parts are made where they are used)
             }
 #pragma unroll
+            for (int it2 = 0; it2 < IT; ++it2)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) none = fmaf(acc[it2][n][r], 0.0f, none);
+            if (none != none) flags[2] = 1;
+#pragma unroll
             for (int it2 = 0; it2 < IT; ++it2) {
                 const int i = 16 * it2 + ln;
                 const float w = reach[i];
@@ -610,6 +626,7 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
 #pragma unroll
                         for (int n = 0; n < NT; ++n) acc[it2][n] = floatx4{0.f, 0.f, 0.f, 0.f};
             __syncthreads();                                 // the scores are there, and the queries are read
+            if (uniform64(flags[2])) break;
             if (nc > 0) fetch_q(next, nc);
         } else if (nc > 0) fetch(next, nc);
 

@@ -161,7 +161,7 @@ def test_infinite_keys_and_values_of_many_steps(dk, dv, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("T", [1100])
+@pytest.mark.parametrize("T", [70, 1100])
 def test_an_infinite_state_outlives_powers_that_are_zero(T, dtype):
     """A key that is infinite in the first step, decays whose powers over 64 steps are no numbers any more: the state that
     comes back is infinite, of the sign that its steps give it."""
@@ -173,3 +173,86 @@ def test_an_infinite_state_outlives_powers_that_are_zero(T, dtype):
         ro, rs, mag, A = ref.decay(q, k, v, g)
         _, state = run(q, k, v, g, dtype)
         same(state, rs, ref.decay_tolerance(ro, mag, rs, A, T, 64, dtype == "bf16")[1])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [9, 70, 1100])
+@pytest.mark.parametrize("dk,dv", DIMS[:4])
+@pytest.mark.parametrize("done", [None, 0.1])
+def test_infinities_of_many_steps_are_the_definitions(dk, dv, T, dtype, done):
+    """Queries and states that came in, too, with and without flags behind them."""
+    check_not_finite(T, dk, dv, dtype, dk + T, done=done)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [20, 64, 1100])
+def test_products_that_overflow_stay_where_they_are(T, dtype):
+    """Finite queries and keys whose products no fp32 number holds: a query and a later key, a query and a key in front of a
+    flag, a query and the key of an earlier step whose value is small, a query and a state that the decay has shrunk."""
+    B, H, d = 4, 1, 64
+    rng, q, k, v, _ = values(T, B, H, d, d, T)
+    done = np.zeros((T, B), np.uint8)
+    q[4, 0], k[9, 0], v[9, 0] = 1e25, 1e25, 1e-20
+    done[10, 0] = 1
+    k[4, 1] = 1e25
+    done[7, 1] = 1
+    q[9, 1] = 1e25
+    k[5, 2], v[5, 2] = 1e22, 1e-22
+    q[12, 2] = 1e22
+    g = np.array([0.01], np.float32).astype(np.float64)
+    s = np.zeros((B, H, d, d), np.float32)
+    s[3] = 1e30
+    q[18, 3] = 1e25
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    ro, rs, mag, A = ref.decay(q, k, v, g, s, done)
+    assert mag.max() < 1e38 and A.max() < 1e38
+    tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, T, d, dtype == "bf16")
+    out, state = run(q, k, v, g, dtype, state=s, done=done)
+    same(state, rs, tol_s)
+    same(out, ro, tol_o)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [40, 1100])
+def test_a_nan_state_ends_at_a_later_flag(T, dtype):
+    rng, q, k, v, g = values(T, 2, 2, 64, 48, T)
+    s = rng.standard_normal((2, 2, 64, 48)).astype(np.float32)
+    s[1] = np.nan
+    done = np.zeros((T, 2), np.uint8)
+    done[17, 1] = 1
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    ro, rs, mag, A = ref.decay(q, k, v, g, s, done)
+    tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, T, 64, dtype == "bf16")
+    out, state = run(q, k, v, g, dtype, state=s, done=done)
+    there = np.isfinite(ro)
+    assert there[17:].all() and not there[:17, 1].any()
+    same(state, rs, tol_s)
+    assert not np.isfinite(out[:17, 1]).any() and (np.abs(out - ro)[there] <= tol_o[there]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("which", "qkv")
+def test_an_infinity_in_every_place_of_a_chunk(which, dtype):
+    """64 steps of 64 dimensions: row b and head h have theirs in step b, dimension h.  The tolerance is one for the sums of
+    all; what is looked at is where the infinities are."""
+    T = B = H = d = 64
+    rng = np.random.default_rng(11)
+    x = {n: rounded(0.25 + rng.random((T, B, H, d)) / 4, dtype) for n in "qkv"}
+    b, h = np.meshgrid(np.arange(B), np.arange(H), indexing="ij")
+    x[which][b, b, h, h] = np.inf
+    g = np.full(H, 0.5)
+    out, state = run(x["q"], x["k"], x["v"], g, dtype)
+    t = np.arange(T)[:, None, None, None]
+    later = np.broadcast_to((t == b[None, :, :, None]) if which == "q" else (t >= b[None, :, :, None]), out.shape)
+    if which == "v":
+        later = later & (np.arange(d) == h[None, :, :, None])
+    assert not np.isnan(out).any() and np.array_equal(np.isinf(out), later)
+    want = np.zeros((B, H, d, d), bool)
+    if which == "k":
+        want[b, h, h, :] = True
+    if which == "v":
+        want[b, h, :, h] = True
+    assert not np.isnan(state).any() and np.array_equal(np.isinf(state), want)
+    other = {n: np.where(np.isinf(a), 0, a) for n, a in x.items()}
+    ro, _ = run(other["q"], other["k"], other["v"], g, dtype)
+    assert np.allclose(out[~later], ro[~later], rtol=2.0 ** -7, atol=0)
