@@ -8,7 +8,8 @@
 //   segment   points == 1: a group is a run of channels; a few lanes own it, sums are shuffles.
 //   resident  a row (or a slice of its groups) fits a workgroup's registers: read once, written once.
 //   split     larger rows: statistics of runs of points, then a second kernel that joins them and reads x again.
-//   plain     what is left (more channels than a workgroup has vectors, points > 1).
+//   plain     what is left: slices of more vectors than the split kernel has threads (a group, or the least run of whole
+//             groups and vectors, of more than 512 of them), one point a row of groups that no workgroup's registers hold.
 #pragma once
 #include <algorithm>
 #include <numeric>
@@ -541,7 +542,9 @@ static inline NormPlan norm_plan(int N, int P, int C, int G, int size, int vec)
         if (cw / vec > 1024 || cw / cg > 2048) break;
         if (C % cw) continue;
         if (cw * size < 128 && cw != C) continue;
-        if (cw / vec <= 256) widest = cw;
+        // split: two points a round where there are such slices, else one (4 rows of 1728 points of 1280 fp32 channels in one
+        // group, 320 vectors: 27 us; by the plain kernel 8.7 ms)
+        if (cw / vec <= NORM_SPLIT_THREADS / 2 || (!widest && cw / vec <= NORM_SPLIT_THREADS)) widest = cw;
         // the widest slice that fits, but narrower ones while the rows alone leave compute units without work
         if (fits(cw, 1024, 8) && (!best || (int64_t)N * (C / cw) >= 256)) best = cw;
     }

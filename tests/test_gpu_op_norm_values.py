@@ -16,3 +16,12 @@ def test_long_groups_far_from_zero(N, P, C, G, mean, spread):
     import torch
     x = mean + spread * torch.randn(N, P, C, device="cuda", generator=torch.Generator("cuda").manual_seed(P))
     check(x, seedinf.group_norm(x, G), G, None, None, "none")
+
+
+@pytest.mark.parametrize("dtype,C,G", [("fp32", 1028, 1), ("fp32", 2048, 1), ("fp32", 511, 1), ("bf16", 4096, 1), ("bf16", 4096, 2), ("bf16", 3600, 3), ("fp32", 333, 1)])
+def test_slices_of_up_to_512_vectors(dtype, C, G):
+    """A row of them that no registers hold: statistics of runs, joined."""
+    import torch
+    x = (2.0 + torch.randn(3, 500, C, device="cuda", generator=torch.Generator("cuda").manual_seed(C))).to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+    w = 1 + 0.1 * torch.randn(C, device="cuda")
+    check(x, seedinf.group_norm(x, G, w, activation="silu"), G, w, None, "silu")

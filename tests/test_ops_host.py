@@ -178,3 +178,9 @@ def test_workspaces_must_not_overlap(lib):
     for name in ("x", "weight", "bias", "out"):
         assert lib.seed_op_group_norm(*dict(a, ws=a[name]).values(), None) == ALIASING, name
     assert lib.seed_op_group_norm(*a.values(), None) == INVALID
+
+
+@pytest.mark.parametrize("dtype,channels,groups", [(0, 1028, 1), (0, 2048, 1), (1, 4096, 1), (0, 333, 1), (1, 511, 1)])
+def test_group_norm_splits_rows_of_wide_slices(lib, dtype, channels, groups):
+    """As many vectors as the splitting kernel has threads, 512: it takes them, and needs a workspace for its statistics."""
+    assert lib.seed_op_group_norm_workspace(dtype, 2, 5000, channels, groups) > 0
