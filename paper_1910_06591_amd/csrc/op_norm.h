@@ -397,16 +397,17 @@ __global__ __launch_bounds__(NORM_SPLIT_THREADS) void norm_stats_kernel(NormArgs
     float* m2 = mean + t.groups;
     const int slice = (int)(blockIdx.x % slices), run = (int)(blockIdx.x / slices % runs);
     const size_t n = blockIdx.x / slices / runs;
-    const int first = run * run_points, last = min(p.P, first + run_points), tile = t.rows * U;
+    // (points are counted in 32 bits without a sign: a round past the last one of 2^31 - 1 stays below 2^32)
+    const uint32_t first = (uint32_t)run * run_points, last = min((uint32_t)p.P, first + run_points), tile = t.rows * U;
     const T* x = (const T*)p.x + n * (size_t)p.P * p.C + slice * cw;
     Pack<T, VEC> d[U], next[U];
     float mu[VEC], sq[VEC], have = 0.0f;                     // of this thread's channels, over `have` points
 #pragma unroll
     for (int e = 0; e < VEC; ++e) mu[e] = sq[e] = 0.0f;
-    norm_tile_load<T, VEC, U>(t, x + (size_t)first * p.C, p.C, last - first, d);
-    for (int at = first; at < last; at += tile) {
-        if (at + tile < last) norm_tile_load<T, VEC, U>(t, x + (size_t)(at + tile) * p.C, p.C, last - at - tile, next);
-        const int left = t.on ? last - at - t.row : 0;       // (u * rows < left: there is a point)
+    norm_tile_load<T, VEC, U>(t, x + (size_t)first * p.C, p.C, (int)(last - first), d);
+    for (uint32_t at = first; at < last; at += tile) {
+        if (at + tile < last) norm_tile_load<T, VEC, U>(t, x + (size_t)(at + tile) * p.C, p.C, (int)(last - at - tile), next);
+        const int left = t.on ? (int)(last - at) - t.row : 0;       // (u * rows < left: there is a point)
         if (left > 0) {
             const float batch = (float)min(U, (left + t.rows - 1) / t.rows), total = have + batch, f = batch / total, inv = 1.0f / batch;
 #pragma unroll
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(NORM_APPLY_THREADS) void norm_apply_kernel(NormArgs
         float cnt = 0.0f, a = 0.0f, b = 0.0f;
         for (int r = lane; r < runs; r += 64) {
             const float2 s = stats[(n * p.G + slice * t.groups + g) * runs + r];
-            norm_join(cnt, a, b, (float)(min(p.P, (r + 1) * run_points) - r * run_points) * (float)cg, s.x, s.y);
+            norm_join(cnt, a, b, (float)min(run_points, p.P - r * run_points) * (float)cg, s.x, s.y);
         }
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -480,10 +481,10 @@ __global__ __launch_bounds__(NORM_APPLY_THREADS) void norm_apply_kernel(NormArgs
     for (int e = 0; e < VEC; ++e) r[e] *= w[e];
     const size_t base = n * (size_t)p.P * p.C + c0, step = (size_t)t.rows * p.C;
     const uint32_t off = t.offset<VEC>(p.C, sizeof(T));
-    const int last = min(p.P, (piece + 1) * part_points);
+    const uint32_t begin = (uint32_t)piece * part_points, last = min((uint32_t)p.P, begin + part_points);
     constexpr int U = 2;                                     // loads in flight
-    for (int first = piece * part_points; first < last; first += U * t.rows) {
-        const int at = first + t.row;
+    for (uint32_t first = begin; first < last; first += U * t.rows) {
+        const uint32_t at = first + t.row;
         const T* x = (const T*)p.x + base + (size_t)first * p.C;
         T* y = (T*)p.y + base + (size_t)first * p.C;
         Pack<T, VEC> d[U];
@@ -535,7 +536,7 @@ static inline NormPlan norm_plan(int N, int P, int C, int G, int size, int vec)
     // Slices of whole groups and whole vectors.  A slice's points are runs of cw * size bytes; below 128 bytes they no
     // longer fill a line of the cache, so smaller slices are taken only if the channels are no more.
     const int unit = std::lcm(cg, vec);
-    auto fits = [&](int cw, int threads, int e) { return cw / vec <= threads && cw / cg <= 2048 && (int64_t)((P + threads / (cw / vec) - 1) / (threads / (cw / vec))) <= e; };
+    auto fits = [&](int cw, int threads, int e) { return cw / vec <= threads && cw / cg <= 2048 && ((int64_t)P + threads / (cw / vec) - 1) / (threads / (cw / vec)) <= e; };
     int best = 0, widest = 0;
     for (int k = 1; k <= C / unit && !(wide && P > 1); ++k) {
         const int cw = unit * k;
@@ -559,13 +560,13 @@ static inline NormPlan norm_plan(int N, int P, int C, int G, int size, int vec)
     // kernel reads them all)
     const int tile = NORM_SPLIT_THREADS / (widest / vec) * NORM_SPLIT_U;
     const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(1, (int64_t)N * (C / widest)));
-    const int64_t runs = std::min<int64_t>(std::min<int64_t>(want, 256), (P + tile - 1) / tile);
+    const int64_t runs = std::min<int64_t>(std::min<int64_t>(want, 256), ((int64_t)P + tile - 1) / tile);
     q.run_points = (int)((P + runs - 1) / runs);
-    q.runs = (P + q.run_points - 1) / q.run_points;
+    q.runs = (int)(((int64_t)P + q.run_points - 1) / q.run_points);
     // second kernel: 512 workgroups of 1024 threads (83 MB read and written: 34 us; 1024 of 512 threads: 40 us)
-    const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(1, (int64_t)N * (C / widest)), (P + 31) / 32));
+    const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(1, (int64_t)N * (C / widest)), ((int64_t)P + 31) / 32));
     q.part_points = (int)((P + pieces - 1) / pieces);
-    q.parts = (P + q.part_points - 1) / q.part_points;
+    q.parts = (int)(((int64_t)P + q.part_points - 1) / q.part_points);
     q.workspace = (size_t)N * q.runs * G * sizeof(float2);
     return q;
 }

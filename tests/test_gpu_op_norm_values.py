@@ -25,3 +25,21 @@ def test_slices_of_up_to_512_vectors(dtype, C, G):
     x = (2.0 + torch.randn(3, 500, C, device="cuda", generator=torch.Generator("cuda").manual_seed(C))).to(torch.float32 if dtype == "fp32" else torch.bfloat16)
     w = 1 + 0.1 * torch.randn(C, device="cuda")
     check(x, seedinf.group_norm(x, G, w, activation="silu"), G, w, None, "silu")
+
+
+@pytest.mark.parametrize("P", [(1 << 31) - 1, (1 << 31) - 1030])
+def test_the_longest_rows(P):
+    """Statistics in 64 bits over a row of 2^31 - 1 points, and its first and last outputs."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    x = torch.empty(1, P, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(5))
+    x += 2
+    y = seedinf.group_norm(x, 1, out=torch.zeros_like(x))
+    parts = x.view(-1).split(1 << 27)
+    mean = sum(float(c.double().sum()) for c in parts) / P
+    var = sum(float((c.double() - mean).square().sum()) for c in parts) / P
+    for at in (slice(0, 3000), slice(P // 2, P // 2 + 3000), slice(P - 3000, P)):
+        want = ((x[0, at, 0].double() - mean) / np.sqrt(var + 1e-5)).cpu().numpy()
+        mag = 8 / np.sqrt(var) + np.abs(want)
+        assert (np.abs(y[0, at, 0].double().cpu().numpy() - want) <= ref.group_norm_tolerance(want, mag, True)).all()

@@ -180,6 +180,11 @@ def test_workspaces_must_not_overlap(lib):
     assert lib.seed_op_group_norm(*a.values(), None) == INVALID
 
 
+def test_the_longest_group_norm_row_is_split(lib):
+    """2^31 - 1 points of one channel: rounds past the last point do not wrap."""
+    assert lib.seed_op_group_norm_workspace(1, 1, (1 << 31) - 1, 1, 1) > 0
+
+
 @pytest.mark.parametrize("dtype,channels,groups", [(0, 1028, 1), (0, 2048, 1), (1, 4096, 1), (0, 333, 1), (1, 511, 1)])
 def test_group_norm_splits_rows_of_wide_slices(lib, dtype, channels, groups):
     """As many vectors as the splitting kernel has threads, 512: it takes them, and needs a workspace for its statistics."""
