@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256, (DecayLds<T, DK, DVT, OUT>::RESIDENT)) void de
     const int hk = id % p.KV, b = id / p.KV, h = hk * grp + hg;
     const int bh = b * p.H + h, col0 = tile * DVT;
     const int len = decay_length(p, b);
-    const int begin = seg * p.segment_steps, end = min(len, begin + p.segment_steps);
+    const int begin = seg * p.segment_steps, end = begin + min(p.segment_steps, len - begin);      // (not behind `begin`: none)
     const bool split = p.segments > 1;
     if (OUT && split && begin >= end) return;                // (the scan has the state)
 
@@ -805,7 +805,7 @@ static inline DecayPlan decay_plan(int dtype, int T, int B, int H, int dk, int d
     const int64_t n = want < most ? want : most;
     if (n > 1) {
         const int steps = (int)(((T + n - 1) / n + C - 1) / C * C);
-        q.segments = (T + steps - 1) / steps; q.segment_steps = steps;
+        q.segments = (int)(((int64_t)T + steps - 1) / steps); q.segment_steps = steps;
     }
     if (q.segments > 1) {
         q.factor_at = ((size_t)B * H * q.segments * dk * dv * sizeof(float) + 255) / 256 * 256;

@@ -256,3 +256,23 @@ def test_an_infinity_in_every_place_of_a_chunk(which, dtype):
     other = {n: np.where(np.isinf(a), 0, a) for n, a in x.items()}
     ro, _ = run(other["q"], other["k"], other["v"], g, dtype)
     assert np.allclose(out[~later], ro[~later], rtol=2.0 ** -7, atol=0)
+
+
+def test_the_longest_axis():
+    """2^31 - 1 steps of one number: around the last segments' borders and at the end, where the decay has forgotten what
+    lies 100 steps back (0.5^100)."""
+    import torch
+    T, n = (1 << 31) - 1, 400
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    gen = torch.Generator("cuda").manual_seed(3)
+    q, k, v = (torch.empty(T, 1, 1, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(3))
+    g = torch.tensor([0.5], device="cuda")
+    out, state = seedinf.decay_attention(q, k, v, g)
+    for end in (n, T // 2, 510 << 22, (511 << 22) + n // 2, T):
+        part = slice(end - n, end)
+        ro, rs, mag, A = ref.decay(*(x[part].double().cpu().numpy() for x in (q, k, v)), np.array([0.5]))
+        tol_o, tol_s = ref.decay_tolerance(ro, mag, rs, A, n, 1, True)
+        late = slice(0 if end == n else 100, n)
+        assert (np.abs(out[part].double().cpu().numpy() - ro)[late] <= tol_o[late] + 1e-28).all(), end
+    assert (np.abs(state.double().cpu().numpy() - rs) <= tol_s + 1e-28).all()

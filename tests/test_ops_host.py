@@ -189,3 +189,10 @@ def test_the_longest_group_norm_row_is_split(lib):
 def test_group_norm_splits_rows_of_wide_slices(lib, dtype, channels, groups):
     """As many vectors as the splitting kernel has threads, 512: it takes them, and needs a workspace for its statistics."""
     assert lib.seed_op_group_norm_workspace(dtype, 2, 5000, channels, groups) > 0
+
+
+@pytest.mark.parametrize("steps", [(1 << 31) - 1, (1 << 31) - (1 << 22) + 1, 1 << 30])
+def test_the_longest_axis_is_split(lib, steps):
+    """512 segments of a state of one number and a pair of factors, whatever is added to the steps to round them up."""
+    n = lib.seed_op_decay_workspace(C.byref(decay_desc(steps=steps, rows=1, heads=1, kv_heads=1, key_dim=1, value_dim=1)))
+    assert 512 * 8 <= n <= 512 * 12 + 256
