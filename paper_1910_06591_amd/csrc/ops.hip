@@ -121,6 +121,8 @@ extern "C" seed_status_t seed_op_decay(const seed_decay_t* d, const void* q, con
     const size_t need = seed_op_decay_workspace(d);
     if (need && (op_overlap(workspace, need, state_in, state_bytes) || op_overlap(workspace, need, state_out, state_bytes)))
         return op_fail(SEED_ERR_ALIASING, "the workspace overlaps a state");
+    for (const auto& a : small)
+        if (op_overlap(a.p, a.bytes, workspace, need)) return op_fail(SEED_ERR_ALIASING, "the workspace overlaps decay, done or lengths");
     if (d->steps > 0) {
         const StridedArray arrays[] = {{out, d->out_step, d->out_row, (int64_t)d->heads * d->value_dim},
                                        {q, d->q_step, d->q_row, (int64_t)d->heads * d->key_dim},

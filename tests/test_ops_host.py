@@ -196,3 +196,11 @@ def test_the_longest_axis_is_split(lib, steps):
     """512 segments of a state of one number and a pair of factors, whatever is added to the steps to round them up."""
     n = lib.seed_op_decay_workspace(C.byref(decay_desc(steps=steps, rows=1, heads=1, kv_heads=1, key_dim=1, value_dim=1)))
     assert 512 * 8 <= n <= 512 * 12 + 256
+
+
+@pytest.mark.parametrize("name", ["decay", "done", "lengths"])
+def test_decay_workspace_must_not_overlap_small_inputs(lib, name):
+    desc = decay_desc(steps=4096, rows=1, heads=1, kv_heads=1, key_dim=64, value_dim=64)
+    n = lib.seed_op_decay_workspace(C.byref(desc))
+    st, msg = decay_call(lib, desc, **dict(FAR, **{name: 7 << 30}), ws=7 << 30, n=n)
+    assert st == ALIASING and "workspace" in msg
