@@ -35,6 +35,9 @@ static bool op_overlap(const void* a, size_t na, const void* b, size_t nb)
     return a && b && na && nb && pa < pb + nb && pb < pa + na;
 }
 
+// n places `stride` elements apart: do they end within 2^46 elements, so that no sum of two such extents leaves 64 bits?
+static bool op_reaches(int64_t n, int64_t stride) { return stride >= 0 && (n <= 1 || stride <= ((int64_t)1 << 46) / (n - 1)); }
+
 static bool op_aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 static seed_status_t op_check_workspace(size_t need, const void* workspace, size_t have)
@@ -60,9 +63,10 @@ static seed_status_t decay_check(const seed_decay_t* d)
     if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads) return op_fail(SEED_ERR_INVALID_ARG, "kv_heads must divide heads, both positive");
     if (d->key_dim < 1 || d->key_dim > 256 || d->value_dim < 1 || d->value_dim > 256)
         return op_fail(SEED_ERR_INVALID_ARG, "key_dim and value_dim must be 1 .. 256");
-    const int64_t strides[] = {d->q_step, d->q_row, d->k_step, d->k_row, d->v_step, d->v_row, d->out_step, d->out_row};
-    for (int64_t s : strides)
-        if (s < 0 || s > ((int64_t)1 << 44)) return op_fail(SEED_ERR_INVALID_ARG, "a stride is negative or too large");
+    const int64_t strides[][2] = {{d->q_step, d->q_row}, {d->k_step, d->k_row}, {d->v_step, d->v_row}, {d->out_step, d->out_row}};
+    for (const auto& s : strides)
+        if (s[0] > ((int64_t)1 << 44) || s[1] > ((int64_t)1 << 44) || !op_reaches(d->steps, s[0]) || !op_reaches(d->rows, s[1]))
+            return op_fail(SEED_ERR_INVALID_ARG, "a stride is negative or too large");
     // a launch's threads stay below 2^32
     if ((int64_t)d->rows * d->heads > ((int64_t)1 << 21)) return op_fail(SEED_ERR_INVALID_ARG, "rows * heads is more than 2^21");
     return SEED_OK;
@@ -247,7 +251,7 @@ seed_status_t seedinf::op_sample_check(int32_t dtype, int32_t rows, int32_t choi
 {
     seed_status_t st = sample_check(dtype, rows, choices);
     if (st != SEED_OK) return st;
-    if (row_stride < 0 || row_stride > (int64_t)1 << 44) return op_fail(SEED_ERR_INVALID_ARG, "row_stride is negative or too large");
+    if (row_stride > (int64_t)1 << 44 || !op_reaches(rows, row_stride)) return op_fail(SEED_ERR_INVALID_ARG, "row_stride is negative or too large");
     if (rows == 0) return SEED_OK;
     if (!logits || !uniforms || !token_out) return op_fail(SEED_ERR_INVALID_ARG, "logits, uniforms and token_out are required");
     const size_t size = op_dtype_size(dtype), bytes = ((size_t)(rows - 1) * row_stride + choices) * size, row4 = (size_t)rows * 4;

@@ -204,3 +204,15 @@ def test_decay_workspace_must_not_overlap_small_inputs(lib, name):
     n = lib.seed_op_decay_workspace(C.byref(desc))
     st, msg = decay_call(lib, desc, **dict(FAR, **{name: 7 << 30}), ws=7 << 30, n=n)
     assert st == ALIASING and "workspace" in msg
+
+
+@pytest.mark.parametrize("kw", [dict(steps=(1 << 21) + 1, q_step=1 << 43), dict(steps=1 << 30, v_step=1 << 40), dict(steps=1 << 30, out_step=1 << 34), dict(rows=1 << 19, k_row=1 << 44)])
+def test_decay_refuses_strides_that_leave_64_bits(lib, kw):
+    """Each stride is one that is allowed; the last step or row would lie further on than an address reaches."""
+    st, msg = decay_call(lib, decay_desc(**dict(dict(heads=1, kv_heads=1), **kw)), **FAR)
+    assert st == INVALID and "stride" in msg
+
+
+def test_sample_refuses_strides_that_leave_64_bits(lib):
+    assert lib.seed_op_sample(*dict(SAMPLE, rows=1 << 21, stride=1 << 44).values(), None) == INVALID
+    assert "row_stride" in lib.seed_op_last_error().decode()
