@@ -519,7 +519,8 @@ seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, in
  * and never fewer than one choice.  The result is the first choice of the order
  * at which the running sum of m exceeds uniform * (the sum over the kept ones).
  * Masses are computed, added and compared in 64 bits (each good to 2^-37 of its
- * value), in an order that does not depend on the run.
+ * value, or, in rows of up to 64 choices, to 2^-57 of the largest one's), in an
+ * order that does not depend on the run.
  *
  *   logits       [rows, choices], `row_stride` elements (not negative) between rows
  *   uniforms     [rows] fp32 in [0, 1) (values outside are clamped, NaN is 0)

@@ -10,8 +10,8 @@
 //          collects those bins' choices, which are sorted and searched.  A row that top-k or min-p leaves few choices is
 //          read once: those go into a list that takes the row's place.
 //          Where the bins hold more choices than fit (logits that are all but equal), the questions are answered one
-//          by one instead, by radix searches over the row (sample_find; 64 x 50001 within a hundredth of a temperature:
-//          190 us, with top-p 290, where spread logits take 40).
+//          by one instead, by radix searches in a bin (sample_find, over the row, with the histogram's masses; 64 x 50001
+//          within a hundredth of a temperature: 151 us, with top-p 217, where spread logits take 40).
 // What bounds a row: the operations in 64 bits and the LDS additions of the first pass, then some twenty dependent phases
 // of 1 - 3 us; few rows leave most compute units idle (64 x 50001 bf16: 44 - 53 us; 4 x 32000 fp32, top-k 50: 24 us).  256 rows of
 // 131072 fp32, top-k 1000: 70 us, 1.9 TB/s.  4096 rows of 18: 5.4 us, a launch's own time.
@@ -33,7 +33,6 @@ struct SampleArgs {
     const float* min_p;                          // [rows] or nullptr; <= 0 or NaN: off
     int32_t* token; float* logprob;              // logprob may be nullptr
     int rows, V;
-    int shift;                                   // V * 2^shift < 2^63
 };
 
 // NaN never wins, and the two zeros are one value.
@@ -211,100 +210,6 @@ template <class T> struct SampleMem {
     template <int NT, int U> __device__ __forceinline__ int tiles() const { return max(1, (vecs + NT * U - 1) / (NT * U)); }
 };
 
-// ---- radix searches: right for every row, several passes a question ----
-
-struct SampleRow {
-    float top;                   // the largest logit
-    double inv_t;
-    double unit;                 // 2^shift
-    // the equal of an infinite largest logit has mass 1, a masked choice none at any temperature
-    __device__ __forceinline__ double exponent(float x) const { return x == top ? 0.0 : (x == -INFINITY ? -INFINITY : ((double)x - (double)top) * inv_t); }
-    __device__ __forceinline__ double mass(float x) const { return exp(exponent(x)); }
-    __device__ __forceinline__ uint64_t units(double m) const { return (uint64_t)(m * unit + 0.5); }
-};
-
-// One place of the order: the first element at which the running count reaches `count` (mass = false), or the running mass
-// reaches (strict = false) or exceeds (strict = true) `limit`.  Returns its key.  There has to be one.
-// Digits of the key from the top, up to 11 bits a pass over the row: three for the logit, those that V needs for the index.
-// A thread adds its choices up while they have the same digit (in rows of equal logits all have).
-template <class T, int NT>
-__device__ __forceinline__ uint64_t sample_find(const SampleMem<T>& x, SampleRow row, bool mass, bool strict, uint64_t count, double limit,
-                                                uint64_t* hist, uint64_t* scratch)
-{
-    const int tid = threadIdx.x, index_bits = 32 - __builtin_clz(max(x.V - 1, 1));
-    uint64_t prefix = 0, before = 0;
-    int low = 64;                                            // key bits below `low` are not yet known
-    while (low > 0) {
-        if (low == 32 && index_bits < 32) {                  // (the index is inverted: ones above its bits)
-            prefix = prefix << (32 - index_bits) | ((1ull << (32 - index_bits)) - 1);
-            low = index_bits;
-        }
-        const int w = low > 32 ? min(SAMPLE_BITS, low - 32) : min(SAMPLE_BITS, low), at = low - w, bins = 1 << w;
-        __syncthreads();                                     // (the previous pass's readers are done)
-        for (int i = tid; i < SAMPLE_BINS; i += NT) hist[i] = 0;
-        __syncthreads();
-        int digit = 0;
-        uint64_t sum = 0;
-        x.template sweep<NT, 2>(0, x.template tiles<NT, 2>(), [&](float f, int i) {
-            f = sample_clean(f);
-            const uint64_t key = sample_key(f, i);
-            if (low < 64 && (key >> low) != prefix) return;
-            const int d = bins - 1 - (int)((key >> at) & (bins - 1));        // (larger keys first)
-            if (d != digit) {
-                if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
-                digit = d; sum = 0;
-            }
-            sum += mass ? row.units(row.mass(f)) : 1;
-        });
-        if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
-        __syncthreads();
-        sample_scan<NT, SAMPLE_BINS / NT>(hist, SAMPLE_BINS, scratch);
-        const int d = sample_first_of(0, bins, bins - 1, [&](int b) {
-            const uint64_t run = before + hist[b];
-            return mass ? (strict ? (double)run > limit : (double)run >= limit) : run >= count;
-        });
-        if (d > 0) before += hist[d - 1];
-        prefix = prefix << w | (uint64_t)(bins - 1 - d);
-        low = at;
-    }
-    __syncthreads();
-    return prefix;
-}
-
-// The filters and the draw of one row by such searches.  hist: SAMPLE_BINS values; best: the first key of the order.
-template <class T, int NT>
-__device__ __forceinline__ void sample_by_search(const SampleArgs& p, int r, const SampleMem<T>& x, SampleRow row, uint64_t best, int k, float top_p, float min_p, float u,
-                                                 uint64_t* hist, uint64_t* scratch)
-{
-    const int tid = threadIdx.x;
-    uint64_t last = 0;                                       // the last kept key
-    double z = 0.0;
-    // top-k, top-p, the draw: one after the other, by one piece of code
-    for (int question = k > 0 ? 0 : top_p < 1.0f ? 1 : 2; question < 3; question = question == 0 && top_p < 1.0f ? 1 : question < 2 ? 2 : 3) {
-        double limit = 0.0;
-        if (question > 0) {
-            const double least = question == 2 && min_p > 0.0f ? (double)min_p : 0.0;
-            uint64_t s = 0;
-            x.template sweep<NT, 2>(0, x.template tiles<NT, 2>(), [&](float f, int i) {
-                f = sample_clean(f);
-                const uint64_t key = sample_key(f, i);
-                if (key < last) return;
-                const double m = row.mass(f);
-                if (m >= least || key == best) s += row.units(m);
-            });
-            z = (double)sample_reduce<NT>(s, scratch, [](uint64_t a, uint64_t b) { return a + b; });
-            limit = (question == 1 ? (double)top_p : (double)u) * z;
-        }
-        const uint64_t at = question == 1 && !(limit > 0.0) ? best : sample_find<T, NT>(x, row, question > 0, question == 2, (uint64_t)k, limit, hist, scratch);
-        if (question < 2) last = at > last ? at : last;
-        else if (tid == 0) {
-            const int i = min((int)(~(uint32_t)at & 0x7fffffffu), p.V - 1);
-            p.token[r] = i;
-            if (p.logprob) p.logprob[r] = (float)(row.exponent(sample_clean((float)x.x[i])) - log(z / row.unit));
-        }
-    }
-}
-
 // ---- a workgroup a row ----
 
 // The histogram's bins, from the first of the order on: u = 16 (16 - (x - centre) / T), bin floor(u).  Logits up to 16
@@ -339,6 +244,62 @@ struct SampleBins {
     __device__ __forceinline__ static double edge(int bin) { return exp(16.0 - (bin + 1) * 0.0625) * (1.0 / 274877906944.0); }
     __device__ __forceinline__ static double mass(double v) { return (double)units(v) * edge(bin(v)); }
 };
+
+// ---- radix searches: where a bin holds more choices than the list, several passes a question ----
+
+// One place of the order inside bin `bin`: the first choice at which the running count (mass = false) reaches `count`, or
+// the bin's running mass, in the bin's units, makes reached(units) true; the bin's last choice if there is none.  Returns its
+// key; `upto`: the count or the units up to and with it, 0 if the bin has no choice.  value(f): what a logit counts as.
+// Digits of the key from the top, up to 11 bits a pass over the row: three for the logit, those that V needs for the index.
+// A thread adds its choices up while they have the same digit (in rows of equal logits all have).
+template <class T, int NT, class V, class F>
+__device__ __forceinline__ uint64_t sample_find(const SampleMem<T>& x, const SampleBins& bins, int bin, bool mass, uint64_t count, V value, F reached,
+                                                uint64_t* hist, uint64_t* scratch, uint64_t& upto)
+{
+    const int tid = threadIdx.x, index_bits = 32 - __builtin_clz(max(x.V - 1, 1));
+    uint64_t prefix = 0, before = 0;
+    int low = 64;                                            // key bits below `low` are not yet known
+    while (low > 0) {
+        if (low == 32 && index_bits < 32) {                  // (the index is inverted: ones above its bits)
+            prefix = prefix << (32 - index_bits) | ((1ull << (32 - index_bits)) - 1);
+            low = index_bits;
+        }
+        const int w = low > 32 ? min(SAMPLE_BITS, low - 32) : min(SAMPLE_BITS, low), at = low - w, digits = 1 << w;
+        __syncthreads();                                     // (the previous pass's readers are done)
+        for (int i = tid; i < SAMPLE_BINS; i += NT) hist[i] = 0;
+        __syncthreads();
+        int digit = 0;
+        uint64_t sum = 0;
+        x.template sweep<NT, 2>(0, x.template tiles<NT, 2>(), [&](float f, int i) {
+            f = value(f);
+            const uint64_t key = sample_key(f + 0.0f, i);
+            if (low < 64 && (key >> low) != prefix) return;
+            const double v = mass || low > 32 ? bins.place(f) : 0.0;
+            if (low > 32 && bins.bin(v) != bin) return;      // (with the logit's digits known, all are in the bin)
+            const int d = digits - 1 - (int)((key >> at) & (digits - 1));    // (larger keys first)
+            if (d != digit) {
+                if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
+                digit = d; sum = 0;
+            }
+            sum += mass ? bins.units(v) : 1;
+        });
+        if (sum) atomicAdd((unsigned long long*)&hist[digit], (unsigned long long)sum);
+        __syncthreads();
+        sample_scan<NT, SAMPLE_BINS / NT>(hist, SAMPLE_BINS, scratch);
+        const uint64_t all = hist[digits - 1];
+        if (all == 0) { upto = 0; __syncthreads(); return 0; }
+        const int d = sample_first_of(0, digits, digits - 1, [&](int b) {
+            const uint64_t run = before + hist[b];
+            return hist[b] == all || (mass ? reached(run) : run >= count);
+        });
+        upto = before + hist[d];
+        if (d > 0) before += hist[d - 1];
+        prefix = prefix << w | (uint64_t)(digits - 1 - d);
+        low = at;
+    }
+    __syncthreads();
+    return prefix;
+}
 
 template <int CAP> struct SampleLds {
     uint64_t hist[SAMPLE_BINS + 64];                         // masses; then, as doubles, their running sums (64 places for what is in no bin)
@@ -626,12 +587,56 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     }
     __syncthreads();
     const int n = l.n;
-    if (n > CAP) {                                           // (uniform)
-        SampleRow sr;
-        sr.top = top; sr.inv_t = bins.inv_t; sr.unit = (double)(1ull << p.shift);
+    if (n > CAP) {                                           // (uniform): the questions below, answered by searches in the bins
+        uint64_t* const hist = l.list;                       // (the list and its running sums: 2048 places at least)
+        static_assert(2 * CAP >= SAMPLE_BINS, "");
+        auto as = [&](float f) { f = sample_clean(f); return inf_row ? (f == INFINITY ? 0.0f : -INFINITY) : f; };
+        auto units_of = [&](int b, auto counts) {            // of the choices of bin b that counts(key, place) holds for
+            uint64_t sum = 0;
+            row.template sweep<NT, 2>(0, row.template tiles<NT, 2>(), [&](float f, int i) {
+                f = as(f);
+                const double v = bins.place(f);
+                if (bins.bin(v) == b && counts(sample_key(f + 0.0f, i), v)) sum += bins.units(v);
+            });
+            return (double)sample_reduce<NT>(sum, l.scratch, [](uint64_t a, uint64_t b) { return a + b; });
+        };
+        double z = z_all;
+        int end = NB;
+        uint64_t upto = 0;
         __syncthreads();
-        const uint64_t best = first_key();
-        sample_by_search<T, NT>(p, r, row, sr, best, k, top_p, min_p, u01, l.hist, l.scratch);
+        if (k_on) {
+            z = zk1; end = kb;
+            if (k_part) {
+                const uint64_t last = sample_find<T, NT>(row, bins, kb, false, (uint64_t)((uint32_t)k - (kb > 0 ? l.count[kb - 1] : 0u)), as,
+                                                         [](uint64_t) { return false; }, hist, l.scratch, upto);
+                z = before(kb) + units_of(kb, [&](uint64_t key, double) { return key >= last; }) * SampleBins::edge(kb);
+            }
+        }
+        if (top_p < 1.0f) {
+            const double limit = (double)top_p * z;
+            const int b = first_bin([&](int b) { return cum[b] >= limit && cum[b] > 0.0; });
+            const double from = before(b), edge = SampleBins::edge(b);
+            sample_find<T, NT>(row, bins, b, true, 0, as, [&](uint64_t run) { return from + (double)run * edge >= limit; }, hist, l.scratch, upto);
+            const double zp = from + (double)upto * edge;
+            if (b < end || (b == end && zp < z)) { end = b; z = zp; }
+        }
+        if (mb < NB - 1 && mb <= end) {
+            const double zm = before(mb) + units_of(mb, [&](uint64_t, double v) { return v <= m_place; }) * SampleBins::edge(mb);
+            if (mb < end || zm < z) { end = mb; z = zm; }
+        }
+        const double one = bins.mass(bins.place(inf_row ? 0.0f : top));
+        if (!(z >= one)) z = one;
+        const double limit = (double)u01 * z;
+        uint64_t key;
+        int b = first_bin([&](int b) { return cum[b] > limit; });
+        do {                                                 // (a running sum's last bit may point behind the last choice)
+            const double from = before(b), edge = SampleBins::edge(b);
+            key = sample_find<T, NT>(row, bins, b, true, 0, as, [&](uint64_t run) { return from + (double)run * edge > limit; }, hist, l.scratch, upto);
+        } while (upto == 0 && b-- > 0);
+        if (tid == 0) {
+            p.token[r] = min((int)(~(uint32_t)key & 0x7fffffffu), p.V - 1);
+            if (p.logprob) p.logprob[r] = (float)log(bins.mass(bins.place(value(key))) / z);
+        }
         return;
     }
     // sort them, larger keys first: up to 256 by counting those in front of each, with several threads for one where there are
@@ -736,6 +741,18 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
 }
 
 // ---- up to 64 choices: a choice a lane, L lanes a row ----
+
+// What rows of up to 64 choices compute with.
+struct SampleRow {
+    float top;                   // the largest logit
+    double inv_t;
+    double unit;                 // 2^57
+    // the equal of an infinite largest logit has mass 1, a masked choice none at any temperature
+    __device__ __forceinline__ double exponent(float x) const { return x == top ? 0.0 : (x == -INFINITY ? -INFINITY : ((double)x - (double)top) * inv_t); }
+    __device__ __forceinline__ double mass(float x) const { return exp(exponent(x)); }
+    __device__ __forceinline__ uint64_t units(double m) const { return (uint64_t)(m * unit + 0.5); }
+};
+
 template <class T, int L>
 __global__ __launch_bounds__(256) void sample_lanes_kernel(SampleArgs p)
 {
@@ -790,13 +807,6 @@ __global__ __launch_bounds__(256) void sample_lanes_kernel(SampleArgs p)
         p.token[r] = none ? -1 : token;
         if (p.logprob) p.logprob[r] = none ? -INFINITY : greedy ? 0.0f : (float)(e - log((double)z / row.unit));
     }
-}
-
-static inline int sample_shift(int V)
-{
-    int bits = 0;
-    while (((int64_t)1 << bits) <= V) ++bits;            // V < 2^bits
-    return 62 - bits < 52 ? 62 - bits : 52;
 }
 
 constexpr int SAMPLE_SMALL = 8192;       // choices up to which a row is 256 threads' work

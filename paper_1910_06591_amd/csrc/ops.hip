@@ -275,7 +275,7 @@ extern "C" seed_status_t seed_op_sample(int32_t dtype, int32_t rows, int32_t cho
     seed_status_t st = op_sample_check(dtype, rows, choices, row_stride, logits, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out);
     if (st != SEED_OK || rows == 0) return st;
     if ((st = op_check_workspace(seed_op_sample_workspace(dtype, rows, choices), workspace, workspace_bytes)) != SEED_OK) return st;
-    SampleArgs p{logits, row_stride, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, rows, choices, sample_shift(choices)};
+    SampleArgs p{logits, row_stride, uniforms, temperature, top_k, top_p, min_p, token_out, logprob_out, rows, choices};
     const hipError_t e = dtype == SEED_DTYPE_FP32 ? sample_launch<float>(p, (hipStream_t)hip_stream) : sample_launch<__bf16>(p, (hipStream_t)hip_stream);
     if (e != hipSuccess) return op_fail(SEED_ERR_DEVICE, "launch failed: %s", hipGetErrorString(e));
     return op_launched();
