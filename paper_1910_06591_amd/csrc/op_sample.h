@@ -551,9 +551,9 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs p)
     want(fb, fb);
     __syncthreads();
     // In 32 bits a place is within 2^-10 of a bin of what it is in 64 (the centre is a logit), but for temperatures whose
-    // inverse leaves 32 bits.
+    // inverse leaves 32 bits, or so large that logits whose difference does may share the bins.
     const float near_centre = (float)bins.centre, near_b = (float)bins.B;
-    const bool far = !(temp > 1e-30f);
+    const bool far = !(temp > 1e-30f && temp < 1e36f);
     auto near = [&](float f) {
         const int b = (int)fminf(fmaxf(fmaf(near_centre - f, near_b, 256.0f), 0.0f), (float)(NB - 1));
         return (l.near[b >> 5] >> (b & 31) & 1) | far;

@@ -31,3 +31,20 @@ def test_a_leader_above_equal_choices(V, dtype):
             assert abs(t - want) <= (1 + place * 2.0 ** -37 if place >= 0 else 0), (gap, u)
             lw = -math.log(z) - (gap if t != 7 else 0)
             assert abs(lp - lw) <= ref.U32 * abs(lw) + 2.0 ** -36, (gap, u)
+
+
+@pytest.mark.parametrize("V", [200, 9000, 70001])
+@pytest.mark.parametrize("t", [1e37, 3e38])
+def test_logits_whose_difference_leaves_the_type(V, t):
+    """Differences of up to 6e38 at temperatures that they are a few of."""
+    import torch
+    rng = np.random.default_rng(V)
+    R = 16
+    x = rng.uniform(-3.3e38, 3.3e38, (R, V)).astype(np.float32)
+    x[:4, 1:] = -3.3e38
+    x[:4, 0] = 3.3e38
+    a = dict(logits=torch.from_numpy(x).cuda(), uniforms=rng.random(R, dtype=np.float32), temperature=np.full(R, t, np.float32))
+    check(a)
+    check(dict(a, top_p=np.full(R, 0.8, np.float32)))
+    check(dict(a, top_k=np.full(R, V // 2, np.int32)))
+    check(dict(a, min_p=np.full(R, 0.3, np.float32)))
