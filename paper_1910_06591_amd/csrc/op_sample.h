@@ -747,8 +747,8 @@ struct SampleRow {
     float top;                   // the largest logit
     double inv_t;
     double unit;                 // 2^57
-    // the equal of an infinite largest logit has mass 1, a masked choice none at any temperature
-    __device__ __forceinline__ double exponent(float x) const { return x == top ? 0.0 : (x == -INFINITY ? -INFINITY : ((double)x - (double)top) * inv_t); }
+    // the equal of an infinite largest logit has mass 1, what is below it and a masked choice none at any temperature
+    __device__ __forceinline__ double exponent(float x) const { return x == top ? 0.0 : (x == -INFINITY || top == INFINITY ? -INFINITY : ((double)x - (double)top) * inv_t); }
     __device__ __forceinline__ double mass(float x) const { return exp(exponent(x)); }
     __device__ __forceinline__ uint64_t units(double m) const { return (uint64_t)(m * unit + 0.5); }
 };

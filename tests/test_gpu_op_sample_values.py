@@ -48,3 +48,20 @@ def test_logits_whose_difference_leaves_the_type(V, t):
     check(dict(a, top_p=np.full(R, 0.8, np.float32)))
     check(dict(a, top_k=np.full(R, V // 2, np.int32)))
     check(dict(a, min_p=np.full(R, 0.3, np.float32)))
+
+
+@pytest.mark.parametrize("V", [3, 18, 64, 300, 9000, 20000])
+def test_infinite_logits_at_an_infinite_temperature(V):
+    """All finite choices are equal there; beside infinite ones they are none."""
+    import torch
+    x = torch.linspace(-3, 3, V, device="cuda").repeat(6, 1)
+    x[:, 1] = -math.inf
+    x[3:, 0] = x[3:, V - 1] = math.inf
+    u = torch.tensor([0.0, 0.4, 0.99] * 2, device="cuda")
+    token, logprob = seedinf.sample(x, u, temperature=math.inf)
+    finite = [0] + list(range(2, V))
+    order = [V - 1] + list(range(V - 2, 1, -1)) + [0] if V > 2 else [0]
+    want = [order[int(Fraction(float(np.float32(p))) * len(finite))] for p in (0.0, 0.4, 0.99)]
+    assert token.tolist() == want + [0, 0, V - 1]
+    lw = torch.tensor([-math.log(V - 1)] * 3 + [-math.log(2)] * 3, device="cuda", dtype=torch.float64)
+    assert ((logprob.double() - lw).abs() <= ref.U32 * lw.abs() + 1e-11).all()
