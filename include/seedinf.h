@@ -500,7 +500,9 @@ seed_status_t seed_op_decay(const seed_decay_t* desc, const void* q, const void*
  *   activation     SEED_ACT_NONE, SEED_ACT_RELU or SEED_ACT_SILU (v * sigmoid(v))
  *
  * groups divides channels, eps >= 0, points * channels < 2^31, rows * groups <=
- * 2^23.  rows == 0 or points == 0 is a no-op.
+ * 2^23.  rows == 0 or points == 0 is a no-op.  Statistics are fp32 numbers: a
+ * group's sum has to stay below 3.4e38, and a larger sum of squared differences
+ * counts as infinite (the result is then the bias).
  */
 size_t seed_op_group_norm_workspace(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups);
 seed_status_t seed_op_group_norm(int32_t dtype, int32_t rows, int32_t points, int32_t channels, int32_t groups,

@@ -374,7 +374,7 @@ __device__ __forceinline__ void norm_join(float& n, float& mean, float& m2, floa
     if (nb > 0.0f) {
         const float d = meanb - mean, f = nb / total;
         mean = fmaf(d, f, mean);
-        m2 += m2b + d * d * n * f;
+        m2 += fmaf(d * (n * f), d, m2b);         // (in this order zero weights come before what may overflow)
         n = total;
     }
 }
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(NORM_SPLIT_THREADS) void norm_stats_kernel(NormArgs
                 for (int u = 0; u < U; ++u) { const float g = u * t.rows < left ? d[u].get(e) - s : 0.0f; q = fmaf(g, g, q); }
                 const float g = s - mu[e];
                 mu[e] = fmaf(g, f, mu[e]);
-                sq[e] += fmaf(g * g, have * f, q);
+                sq[e] += fmaf(g * (have * f), g, q);
             }
             have = total;
         }
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(NORM_SPLIT_THREADS) void norm_stats_kernel(NormArgs
     __syncthreads();
     norm_of_groups<VEC>(mean, t.on ? t.col * VEC : 0, cg, of);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { const float g = mu[e] - of[e]; s[e] = have > 0.0f ? fmaf(g * g, have, sq[e]) : 0.0f; }
+    for (int e = 0; e < VEC; ++e) { const float g = mu[e] - of[e]; s[e] = have > 0.0f ? fmaf(g * have, g, sq[e]) : 0.0f; }
     norm_group_sums<VEC, NT>(t, s, part, m2);
     for (int g = threadIdx.x; g < t.groups; g += NT)
         stats[(n * p.G + slice * t.groups + g) * runs + run] = make_float2(mean[g], m2[g]);

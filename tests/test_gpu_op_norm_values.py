@@ -43,3 +43,13 @@ def test_the_longest_rows(P):
         want = ((x[0, at, 0].double() - mean) / np.sqrt(var + 1e-5)).cpu().numpy()
         mag = 8 / np.sqrt(var) + np.abs(want)
         assert (np.abs(y[0, at, 0].double().cpu().numpy() - want) <= ref.group_norm_tolerance(want, mag, True)).all()
+
+
+@pytest.mark.parametrize("N,P,C,G", [(6, 1, 512, 4), (6, 400, 32, 4), (1, 30000, 16, 4), (3, 500, 1028, 1), (1, 40, 8192, 1)])
+def test_a_constant_whose_square_overflows(N, P, C, G):
+    """No spread, or one of the mean's last bit: what overflows is not multiplied by a weight of zero, and the result is
+    finite."""
+    import torch
+    x = torch.full((N, P, C), 2.0 ** 84, device="cuda")
+    y = seedinf.group_norm(x, G, bias=torch.randn(C, device="cuda"))
+    assert torch.isfinite(y).all()
