@@ -15,14 +15,26 @@ namespace seedinf {
 // takes them out of registers.)
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// x / (1 + exp(-x)); the reciprocal instruction is good to one unit in the last place
-__device__ __forceinline__ float op_silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+// x / (1 + exp(-x)).  The exponential is 2 to the power t = -x / ln 2; what rounding t loses (2^-24 of t, of which the
+// result would lose as much) is put back by the derivative.  The instructions for 2^t and the reciprocal are good to one unit
+// in the last place: 9 roundings in all.  Results below 2^-118 (x < -87) are zero.  Of a result that is rounded to bf16 T is
+// that type: it does without the correction (2^-16 of the result at the far end, beside 2^-9; 65536 groups of 128 bf16:
+// 10.2 us, with it 10.9).
+template <class T>
+__device__ __forceinline__ float op_silu(float x)
+{
+    if constexpr (sizeof(T) == 2) return x * __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+    const float c = __builtin_amdgcn_fmed3f(x, -88.0f, 128.0f), t = c * -1.44269504088896341f;
+    const float lost = fmaf(t, -1.90465429995776804525e-9f, fmaf(t, 0.693147182464599609375f, c));     // c + t ln 2
+    const float e = __builtin_amdgcn_exp2f(t);
+    return x * __builtin_amdgcn_rcpf(1.0f + fmaf(e, -lost, e));
+}
 
-template <int ACT>
+template <int ACT, class T>
 __device__ __forceinline__ float op_activate(float x)
 {
     if constexpr (ACT == SEED_ACT_RELU) return x < 0.0f ? 0.0f : x;    // (a comparison: NaN stays NaN)
-    else if constexpr (ACT == SEED_ACT_SILU) return op_silu(x);
+    else if constexpr (ACT == SEED_ACT_SILU) return op_silu<T>(x);
     else return x;
 }
 

@@ -55,12 +55,13 @@ __device__ __forceinline__ void norm_keep_packed(Pack<T, VEC>& d)
     }
 }
 
-// d: difference to the mean, a: weight over the deviation
+// d: difference to the mean, a: weight over the deviation; T: what the result is rounded to
+template <class T>
 __device__ __forceinline__ float norm_finish(float d, float a, float b, int act)
 {
     const float v = fmaf(d, a, b);
-    if (act == SEED_ACT_RELU) return op_activate<SEED_ACT_RELU>(v);
-    if (act == SEED_ACT_SILU) return op_activate<SEED_ACT_SILU>(v);
+    if (act == SEED_ACT_RELU) return op_activate<SEED_ACT_RELU, T>(v);
+    if (act == SEED_ACT_SILU) return op_activate<SEED_ACT_SILU, T>(v);
     return v;
 }
 
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(256) void norm_plain_kernel(NormArgs p)
     for (int i = wave; i < p.P; i += 4)
         for (int c = lane; c < cg; c += 64) {
             const int ch = g * cg + c;
-            y[(size_t)i * p.C + c] = (T)norm_finish((float)x[(size_t)i * p.C + c] - mean, p.weight ? rstd * p.weight[ch] : rstd, p.bias ? p.bias[ch] : 0.0f, p.act);
+            y[(size_t)i * p.C + c] = (T)norm_finish<T>((float)x[(size_t)i * p.C + c] - mean, p.weight ? rstd * p.weight[ch] : rstd, p.bias ? p.bias[ch] : 0.0f, p.act);
         }
 }
 
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(NORM_SEGMENT_THREADS) void norm_segment_kernel(Norm
         if (c < cg) {
             float f[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = norm_finish(d[i].get(e) - mean, rstd * w[i][e], b[i][e], p.act);
+            for (int e = 0; e < VEC; ++e) f[e] = norm_finish<T>(d[i].get(e) - mean, rstd * w[i][e], b[i][e], p.act);
             *(Pack<T, VEC>*)(y + c) = norm_pack<T, VEC>(f);
         }
     }
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(NT, 8) void norm_resident_kernel(NormArgs p, int cw
             norm_keep_packed(d[i]);
             float f[H];
 #pragma unroll
-            for (int e = 0; e < H; ++e) f[e] = norm_finish(d[i].get(h + e) - mu[e], r[e], b[e], p.act);
+            for (int e = 0; e < H; ++e) f[e] = norm_finish<T>(d[i].get(h + e) - mu[e], r[e], b[e], p.act);
 #pragma unroll
             for (int e = 0; e < H; e += Pack<T, VEC>::SET) d[i].set(h + e, f + e);
         }
@@ -496,7 +497,7 @@ __global__ __launch_bounds__(NORM_APPLY_THREADS) void norm_apply_kernel(NormArgs
             if (at + u * t.rows < last) {
                 float f[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = norm_finish(d[u].get(e) - mu[e], r[e], b[e], p.act);
+                for (int e = 0; e < VEC; ++e) f[e] = norm_finish<T>(d[u].get(e) - mu[e], r[e], b[e], p.act);
                 *(Pack<T, VEC>*)((char*)(y + u * step) + off) = norm_pack<T, VEC>(f);
             }
     }

@@ -53,3 +53,22 @@ def test_a_constant_whose_square_overflows(N, P, C, G):
     x = torch.full((N, P, C), 2.0 ** 84, device="cuda")
     y = seedinf.group_norm(x, G, bias=torch.randn(C, device="cuda"))
     assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("P", [1, 40])
+def test_silu_is_good_to_its_last_bits(P):
+    """A weight of zero: the result is the bias' silu, for every bias from -110 to 60, to 9 roundings of 2^-24 (two are the
+    instructions' for the power and the reciprocal, which are good to a unit, and count twice: 11), or to 2^-118, below which
+    it is zero."""
+    import torch
+    C = 16384
+    b = np.linspace(-110, 60, C).astype(np.float32)
+    x = torch.randn(2, P, C, device="cuda")
+    y = seedinf.group_norm(x, 64, torch.zeros(C, device="cuda"), torch.from_numpy(b).cuda(), activation="silu")
+    v = b.astype(np.longdouble)
+    want = v / (1 + np.exp(-v))
+    err = np.abs(y.cpu().numpy().astype(np.longdouble) - want)
+    assert (err <= 11 * ref.U32 * np.abs(want) + 2.0 ** -118).all(), np.max(err / np.maximum(np.abs(want), 1e-35)) / ref.U32
+    ends = torch.tensor([[np.inf, -np.inf, np.nan, -1e30, 1e30, 0.0, -0.0, -200.0]], dtype=torch.float32, device="cuda")
+    y = seedinf.group_norm(torch.randn(1, 8, device="cuda"), 1, torch.zeros(8, device="cuda"), ends[0], activation="silu")[0]
+    assert y[0] == np.inf and torch.isnan(y[1:3]).all() and y[4] == ends[0, 4] and (y[[3, 5, 6, 7]] == 0).all()
