@@ -39,9 +39,10 @@ __device__ __forceinline__ int decay_length(const DecayArgs& p, int b)
 // workgroups.  A step's o is a sum over dk: 4 rows of a wavefront by shuffles, the 4 wavefronts through LDS.
 // Bound by the state, read and written once: one step of 256 rows, 16 heads of 128 x 128 (537 MB) 101 us, 5.3 TB/s,
 // what a large copy reaches; 8 rows of 4 heads of 64 x 64 4.2 us, a launch's own time.
+// The wavefronts a SIMD are asked for: left alone, the compiler takes twice the registers for 128 rows, and that step 115 us.
 constexpr int DECAY_COLS = 64;
 template <class T, int DK>
-__global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
+__global__ __launch_bounds__(256, DK == 64 ? 8 : DK == 128 ? 6 : 4) void decay_recurrent_kernel(DecayArgs p)
 {
     constexpr int R = DK / 16;                              // rows of the state a thread holds
     __shared__ float sq[DK], sk[DK], sv[DECAY_COLS];
@@ -84,12 +85,23 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(DecayArgs p)
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (ty + 16 * r >= p.dk) continue;              // (a row that is not there: 0 times an infinite value)
             const float kr = sk[ty + 16 * r], qr = sq[ty + 16 * r];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 S[r][j] = fmaf(kr, vv[j], reset ? 0.0f : g * S[r][j]);
                 acc[j] = fmaf(qr, S[r][j], acc[j]);
+            }
+        }
+        // Rows behind key_dim are zero, but 0 times an infinite value is NaN: then they are cleared, and the sums made anew.
+        if (const floatx4 zero = vv * 0.0f; p.dk < DK && !(zero[0] + zero[1] + zero[2] + zero[3] == 0.0f)) {
+            int row = ty;
+            asm volatile("" : "+v"(row));                   // (the rows' conditions are not kept in registers from the loads on)
+            acc = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int r = 0; r < R; ++r, row += 16) {
+                if (row >= p.dk) S[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = fmaf(sq[row], S[r][j], acc[j]);
             }
         }
 #pragma unroll
