@@ -259,7 +259,7 @@ template <class T> __device__ __forceinline__ int decay_place(int d)
     else return (d & ~31) | ((d & 4) << 2) | ((d & 24) >> 1) | (d & 3);
 }
 
-// Steps t0 .. stop as the recurrence says, on the state of DVT columns in memory: a thread has a column and every RG-th row.
+// Steps t0 .. stop as the recurrence says, on the state of DVT columns in memory: a thread has a column and R of its rows.
 // Returns the power of the decay over them, and 1 if a flag lies among them.
 template <class T, int DK, int DVT, bool OUT>
 __device__ __forceinline__ float2 decay_walk(char* lds, const T* q, const T* k, const T* v, T* o, float* state, const uint8_t* done, float g, float scale,
@@ -267,26 +267,42 @@ __device__ __forceinline__ float2 decay_walk(char* lds, const T* q, const T* k, 
 {
     constexpr int RG = 256 / DVT, R = DK / RG;
     float* const key = (float*)lds; float* const query = key + DK; float* const part = query + DK;
-    const int tid = threadIdx.x, col = tid % DVT, rg = tid / DVT;
+    const int tid = threadIdx.x, col = tid % DVT, row0 = tid / DVT * R;
     const bool on = col < dvt;
     __syncthreads();                                         // (the state is there, and what LDS holds is read)
     float x[R], factor = 1.0f, cut = 0.0f;
 #pragma unroll
-    for (int i = 0; i < R; ++i) x[i] = on && rg + RG * i < dk ? state[(size_t)(rg + RG * i) * dv + col] : 0.0f;
-    for (int t = t0; t < stop; ++t) {
-        const bool reset = done && done[(int64_t)t * B];
+    for (int i = 0; i < R; ++i) x[i] = on && row0 + i < dk ? state[(size_t)(row0 + i) * dv + col] : 0.0f;
+    float next_k = 0.0f, next_q = 0.0f, next_v = 0.0f;       // a step's elements, on their way while the one before it is worked on
+    bool next_reset = false;
+    auto fetch = [&](int t) {
         if (tid < dk) {
-            key[tid] = (float)k[(int64_t)t * k_t + tid];
-            if (OUT) query[tid] = (float)q[(int64_t)t * q_t + tid];
+            next_k = (float)k[(int64_t)t * k_t + tid];
+            if (OUT) next_q = (float)q[(int64_t)t * q_t + tid];
         }
-        const float val = on ? (float)v[(int64_t)t * v_t + col] : 0.0f;
+        if (on) next_v = (float)v[(int64_t)t * v_t + col];
+        next_reset = done && done[(int64_t)t * B];
+    };
+    fetch(t0);
+    for (int t = t0; t < stop; ++t) {
+        const bool reset = next_reset;
+        const float val = next_v;
+        if (tid < dk) {
+            key[tid] = next_k;
+            if (OUT) query[tid] = next_q;
+        }
         __syncthreads();
+        if (t + 1 < stop) fetch(t + 1);
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (rg + RG * i >= dk) continue;
-            x[i] = fmaf(key[rg + RG * i], val, reset ? 0.0f : g * x[i]);
-            if (OUT) sum = fmaf(query[rg + RG * i], x[i], sum);
+        for (int i = 0; i < R; i += 4) {
+            const floatx4 k4 = *(const floatx4*)(key + row0 + i), q4 = *(const floatx4*)(query + row0 + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (row0 + i + e >= dk) continue;
+                x[i + e] = fmaf(k4[e], val, reset ? 0.0f : g * x[i + e]);
+                if (OUT) sum = fmaf(q4[e], x[i + e], sum);
+            }
         }
         if (reset) cut = 1.0f; else factor *= g;
         if (OUT) part[tid] = sum;
@@ -299,7 +315,7 @@ __device__ __forceinline__ float2 decay_walk(char* lds, const T* q, const T* k, 
         // (`part` is written again behind the next step's first barrier)
     }
 #pragma unroll
-    for (int i = 0; i < R; ++i) if (on && rg + RG * i < dk) state[(size_t)(rg + RG * i) * dv + col] = x[i];
+    for (int i = 0; i < R; ++i) if (on && row0 + i < dk) state[(size_t)(row0 + i) * dv + col] = x[i];
     return make_float2(factor, cut);
 }
 
