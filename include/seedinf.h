@@ -405,7 +405,7 @@ void seed_batcher_destroy(seed_batcher_t* b);
 /* ------------------------------------------------------------------------
  * Stand-alone operators: a recurrent core, a normalisation and a sampler for
  * agents whose network a caller composes beside (or behind) a seed_infer
- * handle.  Forward passes, as everything here.
+ * handle.  Forward passes, as everything here: nothing is kept for a gradient.
  *
  *   - Device pointers of the current HIP device; work is enqueued on
  *     `hip_stream` (NULL = the default stream) and the call returns without

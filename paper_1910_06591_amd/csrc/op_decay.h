@@ -145,15 +145,16 @@ __global__ __launch_bounds__(256, DK == 64 ? 8 : DK == 128 ? 6 : 4) void decay_r
 //
 // Roundings: bf16 inputs are operands as they are.  What is computed between the products (scores, the state as an operand,
 // the weighted values of its update) is fp32 and is split into three bf16 parts whose sum it is, 24 bits, so that nothing
-// is lost (in two parts outputs were 1.0e-4 of their norm off; 4 prompts of up to 4001 steps: 132 us, with two parts 119;
-// 32768 steps of 16 heads: 255 and 232).  fp32 inputs use the fp32 matrix instructions.
+// is lost (in two parts outputs were 1.0e-4 of their norm off, and the split axes below 10 % faster).  fp32 inputs use the
+// fp32 matrix instructions.
 //
-// What bounds it: not the bytes (32768 steps of 16 heads of 128 x 128, bf16: 537 MB are 100 us), but a chunk's phases,
-// each of which waits for the one before it: LDS writes of keys and values with their steps side by side, scores, their
-// split, the products with the state in accumulators.  Two workgroups a compute unit fill one another's gaps as far as
-// registers (256 a lane) and LDS (80 KiB) allow.  Split into 32 segments: what they add to the state 87 us, the scan
-// of the states 19, the outputs 135; 4 prompts of up to 4001 steps in 8 segments: 37 + 17 + 64; fp32, 32 steps of 128 rows
-// of 4 heads of 64 x 64, not split: 13.3 us of which the state's 16.8 MB take 4.
+// What bounds it: 32768 steps of 16 heads of 128 x 128, bf16, are 537 MB (85 us) and, with the parts, 16 MFLOP a chunk for
+// outputs and 6 for the segments' states, 183 GFLOP (150 us at a large matrix product's rate); and a chunk's phases, each of
+// which waits for the one before it: LDS writes of keys and values with their steps side by side, scores, their split, the
+// products with the state in accumulators.  Two workgroups a compute unit fill one another's gaps as far as registers (256
+// a lane) and LDS (80 KiB) allow.  Split into 32 segments: what they add to the state 85 us, the scan of the states 20, the
+// outputs 171; 4 prompts of up to 4001 steps in 8 segments: 37 + 18 + 80; fp32, 32 steps of 128 rows of 4 heads of 64 x 64,
+// not split: 12.9 us of which the state's 16.8 MB take 3; it goes in and out of accumulators in accesses of 4 bytes.
 //
 // From a chunk on in which a key, a value, a score or a query times the state is not finite, a workgroup walks its steps as
 // the recurrence says, on the state in memory.  The products would carry such a value into steps before it and past flags
@@ -813,8 +814,9 @@ struct DecayPlan {
 };
 
 // Steps up to which the recurrence is walked: a step is a chain of two barriers, where a chunk costs the same for one step
-// as for all of its own.  128 rows of 4 heads of 64 x 64: 4.9 us and 0.7 a step, a chunk 12; 64 rows of 16 heads of
-// 128 x 128: 22 us and 2.2 a step, a chunk 49 (bf16), 59 (fp32).
+// as for all of its own.  9 steps walked and as a chunk, us: 128 rows of 4 heads of 64 x 64 15.2 and 12.2 (fp32), 12.3 and
+// 12.1 (bf16); 64 rows of 16 heads of 128 x 128 57.6 and 56.5 (fp32), 55.6 and 47.9 (bf16); 4 rows of them 12.6 and 14.5;
+// 8 rows of 8 heads of 256 x 256 22.8 and 19.4 (bf16).  12 steps: a chunk everywhere.
 constexpr int DECAY_SHORT = 8;
 
 static inline DecayPlan decay_plan(int dtype, int T, int B, int H, int dk, int dv)

@@ -498,6 +498,7 @@ class Batcher:
 
 
 # ---------------------------------------------------------------- stand-alone operators (seed_op_*)
+# Forward passes only: what they return carries no gradient, also where an input requires one.
 
 _ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 
@@ -627,7 +628,7 @@ def decay_attention(q, k, v, decay, state=None, done=None, lengths=None, scale=1
     steps and rows; decay [heads] fp32; state [rows, heads, key_dim, value_dim] fp32 or None (zero); done [steps, rows]
     uint8; lengths [rows] int32: the steps behind a row's length are neither read nor written (`out` is zero there where
     it is allocated here).  Returns out [steps, rows, heads, value_dim] and the state after the last step; `state_out`
-    may be `state` itself."""
+    may be `state` itself.  No gradient."""
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise TypeError("q, k and v must be [steps, rows, heads, dim]")
     return _decay(q.shape[:2], q, k, v, decay, state, done, lengths, scale, out, state_out, stream)
@@ -635,7 +636,7 @@ def decay_attention(q, k, v, decay, state=None, done=None, lengths=None, scale=1
 
 def decay_step(q, k, v, decay, state=None, done=None, scale=1.0, out=None, state_out=None, stream=None):
     """decay_attention for single tokens: q [rows, heads, key_dim], k, v [rows, kv_heads, ...], done [rows], out
-    [rows, heads, value_dim]."""
+    [rows, heads, value_dim].  No gradient."""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise TypeError("q, k and v must be [rows, heads, dim]")
     return _decay(q.shape[:1], q, k, v, decay, state, done, None, scale, out, state_out, stream)
@@ -643,7 +644,7 @@ def decay_step(q, k, v, decay, state=None, done=None, scale=1.0, out=None, state
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", out=None, stream=None):
     """Group normalisation with an activation ("none", "relu", "silu"), channels last (seed_op_group_norm): x [rows, ...,
-    channels] contiguous, fp32 or bf16; weight and bias [channels] fp32.  `out` may be x itself."""
+    channels] contiguous, fp32 or bf16; weight and bias [channels] fp32.  `out` may be x itself.  No gradient."""
     import torch
     lib = load_library()
     dt, dev, shape = _op_dtype(x, "x"), x.device, x.shape
@@ -671,7 +672,7 @@ def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=Non
     """Sampling with temperature, top-k, top-p and min-p from one given uniform a row (seed_op_sample): logits [rows,
     choices] fp32 or bf16 with dense rows, uniforms [rows]; temperature, top_p, min_p [rows] fp32 and top_k [rows] int32,
     each optional, a number standing for that value in every row.  Returns token [rows] int32 and its log-probability
-    among the kept choices [rows] fp32."""
+    among the kept choices [rows] fp32, without a gradient."""
     import torch
     lib = load_library()
     dt, dev = _op_dtype(logits, "logits"), logits.device
