@@ -783,7 +783,9 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs p)
     const uint32_t bh = blockIdx.x / blocks;
     const size_t at = (size_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
     if (at >= state) return;
-    float s = p.s_in ? p.s_in[bh * state + at] : 0.0f;
+    // (where the first step starts anew what is there is not read: if it is no number, the first segment would be walked)
+    const uint32_t b = bh / p.H;
+    float s = p.s_in && !(p.done && decay_length(p, b) > 0 && p.done[b]) ? p.s_in[bh * state + at] : 0.0f;
     float* seg = p.seg_state + (size_t)bh * p.segments * state + at;
     const float2* f = p.seg_factor + (size_t)bh * p.segments;
     const bool forgets = p.decay[bh % p.H] == 0.0f;

@@ -276,3 +276,21 @@ def test_the_longest_axis():
         late = slice(0 if end == n else 100, n)
         assert (np.abs(out[part].double().cpu().numpy() - ro)[late] <= tol_o[late] + 1e-28).all(), end
     assert (np.abs(state.double().cpu().numpy() - rs) <= tol_s + 1e-28).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [7, 40, 1100, 5000])
+def test_a_flag_in_the_first_step_in_place_of_a_state(T, dtype):
+    """Rows that start anew have whatever memory holds for a state: bit for bit what they give from a state of zero.  A row
+    of no steps keeps its state."""
+    rng, q, k, v, g = values(T, 3, 2, 64, 64, T)
+    q, k, v = (rounded(x, dtype) for x in (q, k, v))
+    done = np.zeros((T, 3), np.uint8)
+    done[0] = 1
+    s = rng.standard_normal((3, 2, 64, 64)).astype(np.float32)
+    s[0], s[1] = np.nan, np.inf
+    lengths = np.array([T, T - 1, 0], np.int32)
+    out, state = run(q, k, v, g, dtype, state=s, done=done, lengths=lengths)
+    zero = np.where(np.arange(3)[:, None, None, None] == 2, s, 0)
+    ro, rs = run(q, k, v, g, dtype, state=zero, done=done, lengths=lengths)
+    assert np.array_equal(out, ro) and np.array_equal(state, rs) and np.isfinite(out).all() and np.array_equal(state[2], s[2])
